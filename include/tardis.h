@@ -181,6 +181,84 @@ tardis_status_t tardis_ffn_forward_static(tardis_handle_t handle, const void* x,
 tardis_status_t tardis_gemm_bf16(int32_t M, int32_t N, int32_t K, const void* A, int32_t lda,
                                  const void* B, int32_t ldb, float* C, int32_t ldc, tardis_stream_t stream);
 
+/* The dense product of a feed-forward block that stays unfolded (the paper folds the layers that its layer-level
+ * thresholds allow, Section 5.1.1; the others, and the reference FFN y = W2 act(W1 x + b1) + b2 of Section 3.1
+ * itself, are two such products), with its epilogue in the same launch:
+ *     y[r, j] = act(sum_i x[r, i] W[j, i] + bias[j]) + residual[r, j]
+ * Sums and the epilogue are held in fp32, y is rounded once.
+ *   dtype      of x and W: TARDIS_F32 (plain fp32 multiply-adds) or TARDIS_BF16 (tensor cores, exact products);
+ *   out_dtype  of y and residual: `dtype`, or TARDIS_F32 with bf16 operands (router logits, a last layer's output);
+ *   act        tardis_act_t or TARDIS_ACT_NONE;
+ *   x, W       device, row-major, 16-byte aligned; k, ldx and ldw multiples of 8;
+ *   bias, residual   device or NULL; y: any ldy >= o, any element-aligned start.
+ * y may be residual (in place, with ldr = ldy) and overlaps none of the other inputs.  n = 0 does nothing.  Asynchronous
+ * on `stream`; allocates nothing; nothing is kept; the same bits from run to run.  (Should a wait inside the tensor-core
+ * kernel run out, which no valid call makes happen, the tile concerned is filled with NaN.)
+ * Errors: INVALID_ARG, UNSUPPORTED (driver without tensor-map support; more than 4194240 rows of fp32), CUDA. */
+#define TARDIS_ACT_NONE (-1)
+typedef struct {
+  int64_t n;                  /* rows of x and y (tokens); below 2^31 */
+  int32_t k, o;               /* channels in and out */
+  int32_t dtype, out_dtype, act;
+  const void* x; int64_t ldx; /* [n, k] */
+  const void* W; int64_t ldw; /* [o, k], the nn.Linear layout */
+  const float* bias;          /* [o] */
+  const void* residual; int64_t ldr;   /* [n, o] */
+  void* y; int64_t ldy;       /* [n, o] */
+} tardis_linear_desc_t;
+tardis_status_t tardis_linear(const tardis_linear_desc_t* desc, tardis_stream_t stream);
+
+/* The same product with weights of its own for every group of rows: FFNs that are split over experts (each expert is an
+ * FFN of the kind above).  Rows are grouped by expert, group sizes are ragged and known to the device only (what
+ * tardis_route makes, or any other router):
+ *     f[r, j] = act(sum_i x[row(r), i] W[e][j, i] + bias[e][j])   for offsets[e] <= r < offsets[e + 1]
+ * with row(r) = rows[r], or r without rows.  Without slots, y[r, j] = f[r, j] + residual[r, j]; rows in no group are left as
+ * they were.  With slots and weights the rows return to their tokens:
+ *     y[t, j] = residual[t, j] + sum_{c < top_k} weights[t, c] f[slots[t, c], j]
+ * added in fp32 in the order of c and rounded once; a slot in no group (-1, for instance) adds nothing.
+ *   offsets    device [n_experts + 1], ascending, within 0 .. n_rows (what is not is clamped to the range and to the
+ *              offset before: groups never overlap or leave the outputs, whatever the array holds);
+ *   rows       device [n_rows] or NULL; an index outside 0 .. n_x - 1 reads as a row of zeros;
+ *   W          [n_experts][o, k]: experts stride_w elements apart (a multiple of 8, at least (o - 1) ldw + k);
+ *   work       with slots: device scratch of at least 4 n_rows o bytes, 16-byte aligned, caller-owned (calls that overlap
+ *              in time need one each); else ignored.
+ * Other arguments, alignment, result and errors as for tardis_linear; n_experts <= 1024 (UNSUPPORTED beyond). */
+typedef struct {
+  int64_t n_rows;             /* rows of f: (token, choice) pairs; below 2^31 */
+  int32_t n_experts, k, o;
+  int32_t dtype, out_dtype, act;
+  const void* x; int64_t ldx; int64_t n_x;      /* [n_x, k] */
+  const void* W; int64_t ldw, stride_w;
+  const float* bias;          /* [n_experts, o] */
+  const int32_t* offsets;
+  const int32_t* rows;
+  const void* residual; int64_t ldr;            /* as y */
+  void* y; int64_t ldy;       /* [n_rows, o], with slots [n_tokens, o] */
+  int64_t n_tokens;           /* the rest: with slots only */
+  int32_t top_k;
+  const int32_t* slots;       /* [n_tokens, top_k] */
+  const float* weights;       /* [n_tokens, top_k] */
+  void* work; size_t work_bytes;
+} tardis_grouped_desc_t;
+tardis_status_t tardis_grouped_linear(const tardis_grouped_desc_t* desc, tardis_stream_t stream);
+
+/* The router of such FFNs: per token the top_k experts with the largest logits (the lower index first among equals) and
+ * their weights, and all (token, choice) pairs sorted by expert, the earlier token first.
+ *   logits     device float [n_tokens, n_experts], leading dimension ldl (e.g. tardis_linear with out_dtype TARDIS_F32).  -inf and
+ *              NaN are no candidates (a masked expert, a padded token): a token with fewer candidates than top_k has
+ *              expert -1, weight 0 and slot -1 in its last choices.  Experts at +inf share their token evenly.
+ *   normalise  1: softmax over the chosen experts; 0: over all candidates
+ *   experts    out, device [n_tokens, top_k], largest logit first;  weights   out, device [n_tokens, top_k]
+ *   offsets    out, device [n_experts + 1]: where each expert's rows begin; the last is the number of pairs
+ *   rows       out, device [n_tokens top_k]: the token of every sorted pair; -1 behind the last
+ *   slots      out, device [n_tokens, top_k]: the place of every pair among them
+ *   work       device scratch of 1024 n_experts bytes, caller-owned; may be NULL for up to 128 tokens
+ * 1 <= top_k <= 32, top_k <= n_experts <= 1024, n_tokens top_k < 2^31 (UNSUPPORTED beyond).  Asynchronous on `stream`;
+ * allocates nothing; nothing is kept; the same bits from run to run.  Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+tardis_status_t tardis_route(int64_t n_tokens, int32_t n_experts, int32_t top_k, int32_t normalise, const float* logits, int64_t ldl,
+                             int32_t* experts, float* weights, int32_t* offsets, int32_t* rows, int32_t* slots, void* work,
+                             size_t work_bytes, tardis_stream_t stream);
+
 /* Synchronises the stream of the handle's most recent call, then fills *out
  * (host memory).  Returns TIMEOUT / CORRUPT when the device error word says so. */
 tardis_status_t tardis_stats(tardis_handle_t handle, tardis_stats_t* out);

@@ -19,8 +19,9 @@ LIB_PATH = os.path.join(_PKG, "libtardis.so")
 TARDIS_OK = 0
 TARDIS_F32, TARDIS_BF16 = 0, 1
 TARDIS_ACT_GELU_TANH, TARDIS_ACT_GELU_ERF, TARDIS_ACT_RELU = 0, 1, 2
+TARDIS_ACT_NONE = -1
 
-EXPORTS = ["tardis_fold", "tardis_ffn_forward", "tardis_ffn_forward_static", "tardis_gemm_bf16", "tardis_stats",
+EXPORTS = ["tardis_fold", "tardis_ffn_forward", "tardis_ffn_forward_static", "tardis_gemm_bf16", "tardis_linear", "tardis_grouped_linear", "tardis_route", "tardis_stats",
            "tardis_set_debug_capture", "tardis_export_folded", "tardis_set_path", "tardis_set_deterministic", "tardis_stack_forward", "tardis_build_predictor", "tardis_destroy", "tardis_calibrate",
            "tardis_debug_phase_stamps", "tardis_range_search", "tardis_neuron_thresholds", "tardis_debug_wait_timeout", "tardis_clear_error", "tardis_debug_fail_alloc", "tardis_debug_live_allocations", "tardis_debug_damage_guard",
            "tardis_save", "tardis_load", "tardis_status_string", "tardis_last_error"]
@@ -40,6 +41,23 @@ class FoldDesc(ctypes.Structure):
                 ("pred_bits", ctypes.c_int32), ("pred_group", ctypes.c_int32),
                 ("pred_codes", ctypes.c_void_p), ("pred_scale", ctypes.c_void_p),
                 ("pred_zero", ctypes.c_void_p), ("flags", ctypes.c_uint32)]
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("k", ctypes.c_int32), ("o", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+                ("W", ctypes.c_void_p), ("ldw", ctypes.c_int64), ("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+                ("ldr", ctypes.c_int64), ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64)]
+
+
+class GroupedDesc(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int64), ("n_experts", ctypes.c_int32), ("k", ctypes.c_int32), ("o", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("x", ctypes.c_void_p),
+                ("ldx", ctypes.c_int64), ("n_x", ctypes.c_int64), ("W", ctypes.c_void_p), ("ldw", ctypes.c_int64),
+                ("stride_w", ctypes.c_int64), ("bias", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("rows", ctypes.c_void_p),
+                ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64), ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64),
+                ("n_tokens", ctypes.c_int64), ("top_k", ctypes.c_int32), ("slots", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("work", ctypes.c_void_p), ("work_bytes", ctypes.c_size_t)]
 
 
 class Stats(ctypes.Structure):
@@ -78,6 +96,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.tardis_stack_forward.argtypes = [vp, vp, vp, vp, ctypes.c_size_t, vp, ctypes.c_size_t, ctypes.c_int64, vp]
     lib.tardis_destroy.argtypes = [vp]
     lib.tardis_gemm_bf16.argtypes = [i32, i32, i32, vp, i32, vp, i32, vp, i32, vp]
+    lib.tardis_linear.argtypes = [vp, vp]
+    lib.tardis_grouped_linear.argtypes = [vp, vp]
+    lib.tardis_route.argtypes = [i64, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.tardis_calibrate.argtypes = [i32, i32, vp, i64, vp, ctypes.c_double, ctypes.c_double, i32, vp, vp, vp, vp, vp]
     lib.tardis_debug_phase_stamps.argtypes = [vp, i32]
     lib.tardis_range_search.argtypes = [i32, i32, vp, i64, vp, vp, ctypes.c_double, ctypes.c_double, i32, vp, vp, vp, vp, vp, vp]
@@ -171,6 +192,131 @@ def tardis_gemm_bf16(A: torch.Tensor, B: torch.Tensor, C: torch.Tensor, stream=N
     _check(lib.tardis_gemm_bf16(M, N, K, A.data_ptr(), A.stride(0), B.data_ptr(), B.stride(0), C.data_ptr(), C.stride(0),
                                 _stream(stream)), "tardis_gemm_bf16")
     return C
+
+
+def _rows_of(t: torch.Tensor, name: str, dtype, shape, device):
+    """(data pointer, leading dimension) of a matrix with unit inner stride."""
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise TardisError(1, "%s must be a %s tensor of shape %s on %s with unit inner stride" % (name, dtype, shape, device))
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vector(t: Optional[torch.Tensor], name: str, dtype, shape, device) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
+        raise TardisError(1, "%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, shape, device))
+    return t.data_ptr()
+
+
+def _operand_device(x: torch.Tensor):
+    """x's device, which has to be the current one: that is where the launch goes."""
+    if not x.is_cuda or x.device.index != torch.cuda.current_device():
+        raise TardisError(1, "tensors must lie on the current CUDA device")
+    return x.device
+
+
+def tardis_linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = TARDIS_ACT_NONE,
+                  residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype=None, stream=None):
+    """y = act(x W^T + bias) + residual in one launch (see tardis_linear in tardis.h): x [n, k], W [o, k] float32 or bfloat16
+    with unit inner stride, bias [o] float32, residual and y [n, o] in out_dtype (x's dtype, or float32).  Returns y (`out`
+    when given; it may be the residual)."""
+    dev = _operand_device(x)
+    if x.dim() != 2 or W.dim() != 2 or W.shape[1] != x.shape[1]:
+        raise TardisError(1, "x must be [n, k] and W [o, k]")
+    (n, k), o = x.shape, W.shape[0]
+    if out_dtype is None:
+        out_dtype = x.dtype if out is None else out.dtype
+    if out is None:
+        out = torch.empty(n, o, dtype=out_dtype, device=dev)
+    px, ldx = _rows_of(x, "x", x.dtype, (n, k), dev)
+    pw, ldw = _rows_of(W, "W", x.dtype, (o, k), dev)
+    py, ldy = _rows_of(out, "out", out_dtype, (n, o), dev)
+    pr, ldr = _rows_of(residual, "residual", out_dtype, (n, o), dev) if residual is not None else (None, 0)
+    desc = LinearDesc(n, k, o, _dtype_code(x.dtype), _dtype_code(out_dtype), act, px, ldx, pw, ldw,
+                      _vector(bias, "bias", torch.float32, (o,), dev), pr, ldr, py, ldy)
+    _check(load_library().tardis_linear(ctypes.byref(desc), _stream(stream)), "tardis_linear")
+    return out
+
+
+def _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, back, work, stream, what):
+    dev = _operand_device(x)
+    if x.dim() != 2 or W.dim() != 3 or W.shape[2] != x.shape[1]:
+        raise TardisError(1, "x must be [n, k] and W [experts, o, k]")
+    (nx, k), (experts, o, _) = x.shape, W.shape
+    n = nx if rows is None else rows.numel()
+    if out_dtype is None:
+        out_dtype = x.dtype if out is None else out.dtype
+    slots, weights = back if back is not None else (None, None)
+    if slots is not None and slots.dim() != 2:
+        raise TardisError(1, "slots must be [tokens, top_k]")
+    tokens, top_k = slots.shape if slots is not None else (0, 0)
+    n_out = n if slots is None else tokens
+    if out is None:
+        out = torch.empty(n_out, o, dtype=out_dtype, device=dev)
+    room = 0
+    if slots is not None:
+        room = 4 * n * o
+        if work is None:
+            work = torch.empty(n * o, dtype=torch.float32, device=dev)
+        elif work.device != dev or not work.is_contiguous() or work.numel() * work.element_size() < room:
+            raise TardisError(1, "work must be a contiguous tensor of at least 4 rows o bytes on x's device")
+    px, ldx = _rows_of(x, "x", x.dtype, (nx, k), dev)
+    if W.dtype != x.dtype or W.device != dev or W.stride(2) != 1:
+        raise TardisError(1, "W must have x's dtype and device and unit inner stride")
+    py, ldy = _rows_of(out, "out", out_dtype, (n_out, o), dev)
+    pr, ldr = _rows_of(residual, "residual", out_dtype, (n_out, o), dev) if residual is not None else (None, 0)
+    i32 = torch.int32
+    desc = GroupedDesc(n, experts, k, o, _dtype_code(x.dtype), _dtype_code(out_dtype), act, px, ldx, nx, W.data_ptr(),
+                       W.stride(1) if o > 1 else k, W.stride(0), _vector(bias, "bias", torch.float32, (experts, o), dev),
+                       _vector(offsets, "offsets", i32, (experts + 1,), dev), _vector(rows, "rows", i32, (n,), dev), pr, ldr, py, ldy,
+                       tokens, top_k, _vector(slots, "slots", i32, (tokens, top_k), dev),
+                       _vector(weights, "weights", torch.float32, (tokens, top_k), dev), work.data_ptr() if room else None, room)
+    _check(load_library().tardis_grouped_linear(ctypes.byref(desc), _stream(stream)), what)
+    return out
+
+
+def tardis_grouped_linear(x: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                          act: int = TARDIS_ACT_NONE, rows: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                          out: Optional[torch.Tensor] = None, out_dtype=None, stream=None):
+    """The product of tardis_linear with each group's own weights (see tardis_grouped_linear in tardis.h): W [experts, o, k], bias
+    [experts, o], offsets int32 [experts + 1] on the device; y[r] = act(W_e x[rows[r]] + bias_e) + residual[r] for
+    offsets[e] <= r < offsets[e + 1].  Rows of `out` in no group are left as they were."""
+    return _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, None, None, stream, "tardis_grouped_linear")
+
+
+def tardis_grouped_linear_combine(x: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor,
+                                  bias: Optional[torch.Tensor] = None, act: int = TARDIS_ACT_NONE, rows: Optional[torch.Tensor] = None,
+                                  residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype=None,
+                                  work: Optional[torch.Tensor] = None, stream=None):
+    """tardis_grouped_linear and the weighted return to the tokens: y[t] = residual[t] + sum_c weights[t, c] f[slots[t, c]], slots int32
+    and weights float32 [tokens, top_k].  `work` is scratch of 4 rows o bytes (made here when not given)."""
+    return _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, (slots, weights), work, stream,
+                    "tardis_grouped_linear_combine")
+
+
+def tardis_route(logits: torch.Tensor, top_k: int, normalise: bool = True, stream=None):
+    """The experts of every token (see tardis_route in tardis.h): logits float32 [tokens, experts] with unit inner stride.  Returns
+    (experts int32 [tokens, top_k], weights float32 [tokens, top_k], offsets int32 [experts + 1], rows int32 [tokens top_k],
+    slots int32 [tokens, top_k]): what tardis_grouped_linear and tardis_grouped_linear_combine take."""
+    dev = _operand_device(logits)
+    if logits.dim() != 2:
+        raise TardisError(1, "logits must be [tokens, experts]")
+    n, e = logits.shape
+    pl, ldl = _rows_of(logits, "logits", torch.float32, (n, e), dev)
+    if not 1 <= top_k <= e:
+        raise TardisError(1, "top_k must be between 1 and the number of experts")
+    i32 = torch.int32
+    experts = torch.empty(n, top_k, dtype=i32, device=dev)
+    weights = torch.empty(n, top_k, dtype=torch.float32, device=dev)
+    offsets = torch.empty(e + 1, dtype=i32, device=dev)
+    rows = torch.empty(n * top_k, dtype=i32, device=dev)
+    slots = torch.empty(n, top_k, dtype=i32, device=dev)
+    work = torch.empty(256 * e, dtype=i32, device=dev) if n > 128 else None
+    _check(load_library().tardis_route(n, e, top_k, 1 if normalise else 0, pl, ldl, experts.data_ptr(), weights.data_ptr(),
+                                       offsets.data_ptr(), rows.data_ptr(), slots.data_ptr(), work.data_ptr() if work is not None else None,
+                                       1024 * e if work is not None else 0, _stream(stream)), "tardis_route")
+    return experts, weights, offsets, rows, slots
 
 
 def tardis_calibrate(z: torch.Tensor, b1: Optional[torch.Tensor], q_lo: float, q_hi: float, act: int, stream=None):

@@ -11,6 +11,7 @@
 #include <vector>
 #include "common.cuh"
 #include "gemm.cuh"
+#include "linear.cuh"
 
 namespace tardis {
 
@@ -341,6 +342,95 @@ tardis_status_t tardis_gemm_bf16(int32_t M, int32_t N, int32_t K, const void* A,
   g.A1 = A; g.B1 = B; g.lda1 = lda; g.ldb1 = ldb;
   g.epilogue = GEMM_EPI_F32; g.out_f32 = C; g.ldo = ldc;
   return launch_gemm(g, reinterpret_cast<cudaStream_t>(stream));
+}
+
+// What tardis_linear and tardis_grouped_linear ask of their arguments alike.
+static bool linear_args_ok(const LinearArgs& a, long long n, long long nx, long long out_rows) {
+  constexpr long long kMost = 1ll << 31;
+  if (n < 0 || n >= kMost || nx < 0 || nx >= kMost || out_rows < 0 || out_rows >= kMost || a.k <= 0 || a.o <= 0) return false;
+  if (a.dtype != TARDIS_F32 && a.dtype != TARDIS_BF16) return false;
+  if (a.out_dtype != TARDIS_F32 && a.out_dtype != a.dtype) return false;
+  if (a.act != TARDIS_ACT_NONE && a.act != TARDIS_ACT_GELU_TANH && a.act != TARDIS_ACT_GELU_ERF && a.act != TARDIS_ACT_RELU) return false;
+  constexpr long long kMostLd = 1ll << 36;
+  if (a.k % 8 || a.ldx % 8 || a.ldw % 8 || a.ldx < a.k || a.ldw < a.k || a.ldy < a.o || (a.res && a.ldr < a.o)) return false;
+  return a.ldx <= kMostLd && a.ldw <= kMostLd && a.ldy <= kMostLd && (!a.res || a.ldr <= kMostLd) && a.stride_w <= kMostLd;
+}
+static bool linear_pointers_ok(const LinearArgs& a, long long nx, long long out_rows) {
+  if (!a.x || !a.W || !a.y || !aligned16(a.x) || !aligned16(a.W)) return false;
+  const long long in = a.dtype == TARDIS_BF16 ? 2 : 4, out = a.out_dtype == TARDIS_BF16 ? 2 : 4;
+  auto off = [](const void* p, long long unit) { return (reinterpret_cast<uintptr_t>(p) & (unit - 1)) != 0; };
+  if (off(a.y, out) || off(a.res, out) || off(a.bias, 4)) return false;
+  // y is written while the inputs are still read: nothing but the residual itself may share its memory.  Matrices of the same leading dimension may
+  // lie side by side in one buffer (columns that do not meet); with different ones, areas that reach into each other are refused.
+  const uintptr_t y0 = reinterpret_cast<uintptr_t>(a.y);
+  const long long y_ld = a.ldy * out, y_width = a.o * out;
+  auto meets = [&](const void* p, long long rows, long long ld, long long width) {
+    const uintptr_t p0 = reinterpret_cast<uintptr_t>(p);
+    if (!p || rows <= 0 || p0 >= y0 + (out_rows - 1) * y_ld + y_width || y0 >= p0 + (rows - 1) * ld + width) return false;
+    if (ld != y_ld) return true;
+    const long long apart = ((long long)(p0 - y0) % ld + ld) % ld;      // from the beginning of a row of y to that of the next row of p
+    return apart < y_width || apart + width > ld;
+  };
+  if (meets(a.x, nx, a.ldx * in, a.k * in) || meets(a.bias, a.groups, a.o * 4ll, a.o * 4ll)) return false;
+  if (meets(a.W, 1, 0, ((a.groups - 1) * a.stride_w + (a.o - 1) * a.ldw + a.k) * in)) return false;
+  return !(meets(a.res, out_rows, a.ldr * out, a.o * out) && !(a.res == a.y && a.ldr == a.ldy));
+}
+
+tardis_status_t tardis_linear(const tardis_linear_desc_t* d, tardis_stream_t stream) {
+  if (!d) return TARDIS_ERR_INVALID_ARG;
+  LinearArgs a = {};
+  a.n = a.nx = int(d->n); a.k = d->k; a.o = d->o; a.dtype = d->dtype; a.out_dtype = d->out_dtype; a.act = d->act;
+  a.x = d->x; a.ldx = d->ldx; a.W = d->W; a.ldw = d->ldw; a.bias = d->bias; a.res = d->residual; a.ldr = d->ldr; a.y = d->y; a.ldy = d->ldy;
+  a.groups = 1;
+  if (!linear_args_ok(a, d->n, d->n, d->n)) return TARDIS_ERR_INVALID_ARG;
+  if (d->n == 0) return TARDIS_OK;
+  if (!linear_pointers_ok(a, d->n, d->n)) return TARDIS_ERR_INVALID_ARG;
+  return launch_linear(a, reinterpret_cast<cudaStream_t>(stream));
+}
+
+tardis_status_t tardis_grouped_linear(const tardis_grouped_desc_t* d, tardis_stream_t stream) {
+  if (!d) return TARDIS_ERR_INVALID_ARG;
+  LinearArgs a = {};
+  a.n = int(d->n_rows); a.nx = int(d->n_x); a.k = d->k; a.o = d->o; a.dtype = d->dtype; a.out_dtype = d->out_dtype; a.act = d->act;
+  a.x = d->x; a.ldx = d->ldx; a.W = d->W; a.ldw = d->ldw; a.stride_w = d->stride_w; a.bias = d->bias;
+  a.res = d->residual; a.ldr = d->ldr; a.y = d->y; a.ldy = d->ldy;
+  a.groups = d->n_experts; a.offsets = d->offsets; a.rows = d->rows;
+  const bool back = d->slots || d->weights;
+  const long long out_rows = back ? d->n_tokens : d->n_rows;
+  if (a.groups <= 0 || !linear_args_ok(a, d->n_rows, d->n_x, out_rows)) return TARDIS_ERR_INVALID_ARG;
+  if (a.groups > kMaxExperts) return TARDIS_ERR_UNSUPPORTED;
+  if (a.groups > 1 && (a.stride_w % 8 || a.stride_w < (a.o - 1) * a.ldw + a.k)) return TARDIS_ERR_INVALID_ARG;
+  if (back && (!d->slots || !d->weights || d->top_k <= 0)) return TARDIS_ERR_INVALID_ARG;
+  if (out_rows == 0) return TARDIS_OK;
+  if (!a.offsets || (!a.rows && d->n_x < d->n_rows) || (reinterpret_cast<uintptr_t>(a.offsets) | reinterpret_cast<uintptr_t>(a.rows)) & 3u) return TARDIS_ERR_INVALID_ARG;
+  if (!linear_pointers_ok(a, d->n_x, out_rows)) return TARDIS_ERR_INVALID_ARG;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (!back) return launch_linear(a, s);
+  if ((reinterpret_cast<uintptr_t>(d->slots) | reinterpret_cast<uintptr_t>(d->weights)) & 3u) return TARDIS_ERR_INVALID_ARG;
+  const size_t room = size_t(a.n) * size_t(a.o) * 4;
+  if (room > 0 && (!d->work || !aligned16(d->work) || d->work_bytes < room)) return TARDIS_ERR_INVALID_ARG;
+  LinearArgs f = a;
+  f.res = nullptr; f.y = d->work; f.ldy = a.o; f.out_dtype = TARDIS_F32;
+  if (f.n > 0) {
+    const tardis_status_t st = launch_linear(f, s);
+    if (st != TARDIS_OK) return st;
+  }
+  return launch_combine(int(out_rows), d->top_k, a, static_cast<const float*>(d->work), d->slots, d->weights, s);
+}
+
+tardis_status_t tardis_route(int64_t n_tokens, int32_t n_experts, int32_t top_k, int32_t normalise, const float* logits, int64_t ldl,
+                             int32_t* experts, float* weights, int32_t* offsets, int32_t* rows, int32_t* slots, void* work,
+                             size_t work_bytes, tardis_stream_t stream) {
+  if (n_tokens < 0 || n_experts <= 0 || top_k <= 0 || top_k > n_experts || ldl < n_experts || (normalise != 0 && normalise != 1))
+    return TARDIS_ERR_INVALID_ARG;
+  if (n_experts > kMaxExperts || top_k > 32 || n_tokens >= (1ll << 31) / top_k) return TARDIS_ERR_UNSUPPORTED;
+  if (!offsets || (n_tokens > 0 && (!logits || !experts || !weights || !rows || !slots))) return TARDIS_ERR_INVALID_ARG;
+  const void* all[] = {logits, experts, weights, offsets, rows, slots, work};
+  for (const void* p : all)
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return TARDIS_ERR_INVALID_ARG;
+  if (n_tokens > 128 && (!work || work_bytes < size_t(1024) * size_t(n_experts))) return TARDIS_ERR_INVALID_ARG;
+  return launch_route(int(n_tokens), n_experts, top_k, normalise, logits, ldl, experts, weights, offsets, rows, slots,
+                      static_cast<int*>(work), reinterpret_cast<cudaStream_t>(stream));
 }
 
 tardis_status_t tardis_calibrate(int32_t d_ff, int32_t n_cal, const float* z, int64_t ldz, const float* b1, double q_lo,

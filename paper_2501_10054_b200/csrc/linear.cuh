@@ -1,0 +1,95 @@
+// The dense products of the feed-forward blocks that stay unfolded (internal): what the kernels of linear.cu (any type, few
+// rows) and linear_tc.cu (tensor cores) take.
+//   y[r, o] = act(sum_k x[row(r), k] W_e[o, k] + bias_e[o]) + res[r, o]       e = the group of row r
+#pragma once
+#include "common.cuh"
+
+namespace tardis {
+
+constexpr int kMaxExperts = 1024;
+
+struct LinearArgs {
+  int n, k, o;                       // rows of the output, channels, outputs
+  int dtype, out_dtype, act;         // act: TARDIS_ACT_NONE or one of tardis_act_t
+  const void* x; long long ldx;      // [nx, k]
+  int nx;
+  const void* W; long long ldw, stride_w;      // [groups][o, k]
+  const float* bias;                 // [groups][o] or null
+  const void* res; long long ldr;    // [n, o] in out_dtype or null
+  void* y; long long ldy;
+  int groups;                        // 1 without offsets
+  const int* offsets;                // [groups + 1] or null (one group of all rows)
+  const int* rows;                   // [n] or null: row r of the product takes row rows[r] of x (zeros where that is outside [0, nx))
+};
+
+tardis_status_t launch_linear(const LinearArgs& a, cudaStream_t s);
+// What a gives in fp32 as f [a.n, a.o], returned to the tokens: a.y[t, o] = a.res[t, o] + sum_j weights[t, j] f[slots[t, j], o]; slots outside
+// the groups add nothing
+tardis_status_t launch_combine(int tokens, int top_k, const LinearArgs& a, const float* f, const int* slots, const float* weights,
+                               cudaStream_t s);
+tardis_status_t launch_route(int tokens, int experts, int top_k, int normalise, const float* logits, long long ldl, int* chosen,
+                             float* weights, int* offsets, int* rows, int* slots, int* work, cudaStream_t s);
+
+// ---- device side ----
+// One thread's view of the grouped rows.  Offsets come from device memory: each is clamped to [0, n] and to its predecessors, so whatever
+// they hold, groups are disjoint and inside the output.
+struct GroupTile { int e, first, rows; };     // group, first row of the tile, rows of the tile (0: no such tile)
+
+// Tile `tile` of the sequence that cuts every group into tiles of `per` rows, groups in order, by one converged warp (all lanes get it).
+__device__ __forceinline__ GroupTile find_group_tile(const int* offsets, int groups, int n, int per, int tile) {
+  GroupTile t = {0, 0, 0};
+  if (!offsets) {
+    const long long first = (long long)(tile) * per;
+    if (first < n) { t.first = int(first); t.rows = min(per, n - int(first)); }
+    return t;
+  }
+  const int lane = threadIdx.x & 31;
+  int end = min(max(offsets[0], 0), n), before = 0;          // where the groups so far end, and their tiles
+  for (int e0 = 0; e0 < groups; e0 += 32) {
+    const int e = e0 + lane;
+    int mine = e < groups ? min(max(offsets[e + 1], 0), n) : 0;
+    mine = max(mine, end);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int other = __shfl_up_sync(0xffffffffu, mine, d);
+      if (lane >= d) mine = max(mine, other);
+    }
+    int start = __shfl_up_sync(0xffffffffu, mine, 1);
+    if (lane == 0) start = end;
+    int tiles = (mine - start + per - 1) / per;
+    const int own = tiles;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int other = __shfl_up_sync(0xffffffffu, tiles, d);
+      if (lane >= d) tiles += other;
+    }
+    const int skip = before + tiles - own;                    // tiles in front of this lane's group
+    const unsigned hit = __ballot_sync(0xffffffffu, tile >= skip && tile < skip + own);
+    if (hit) {
+      const int src = __ffs(hit) - 1;
+      const int g_first = __shfl_sync(0xffffffffu, start, src), g_end = __shfl_sync(0xffffffffu, mine, src);
+      t.e = e0 + src;
+      t.first = g_first + (tile - __shfl_sync(0xffffffffu, skip, src)) * per;
+      t.rows = min(per, g_end - t.first);
+      return t;
+    }
+    end = __shfl_sync(0xffffffffu, mine, 31);
+    before += __shfl_sync(0xffffffffu, tiles, 31);
+  }
+  return t;
+}
+
+__device__ __forceinline__ float apply_act(float z, int act) {
+  if (act == TARDIS_ACT_NONE) return z;
+  if (act == TARDIS_ACT_RELU) return z < 0.f ? 0.f : z;              // (of -inf 0, of NaN NaN)
+  return gelu_f32(z, act);
+}
+__device__ __forceinline__ float load_out(const void* p, long long i, int dtype) {
+  return dtype == TARDIS_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : static_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ void store_out(void* p, long long i, int dtype, float v) {
+  if (dtype == TARDIS_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+  else static_cast<float*>(p)[i] = v;
+}
+
+}  // namespace tardis
