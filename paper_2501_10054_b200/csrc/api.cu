@@ -402,7 +402,7 @@ tardis_status_t tardis_grouped_linear(const tardis_grouped_desc_t* d, tardis_str
   if (a.groups > 1 && (a.stride_w % 8 || a.stride_w < (a.o - 1) * a.ldw + a.k)) return TARDIS_ERR_INVALID_ARG;
   if (back && (!d->slots || !d->weights || d->top_k <= 0)) return TARDIS_ERR_INVALID_ARG;
   if (out_rows == 0) return TARDIS_OK;
-  if (!a.offsets || (!a.rows && d->n_x < d->n_rows) || (reinterpret_cast<uintptr_t>(a.offsets) | reinterpret_cast<uintptr_t>(a.rows)) & 3u) return TARDIS_ERR_INVALID_ARG;
+  if (!a.offsets || d->n_x < (a.rows ? 1 : d->n_rows) || (reinterpret_cast<uintptr_t>(a.offsets) | reinterpret_cast<uintptr_t>(a.rows)) & 3u) return TARDIS_ERR_INVALID_ARG;
   if (!linear_pointers_ok(a, d->n_x, out_rows)) return TARDIS_ERR_INVALID_ARG;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (!back) return launch_linear(a, s);

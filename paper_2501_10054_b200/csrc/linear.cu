@@ -97,7 +97,7 @@ tardis_status_t launch_combine(int tokens, int top_k, const LinearArgs& a, const
 
 tardis_status_t launch_linear(const LinearArgs& a, cudaStream_t s) {
   using namespace linear;
-  return a.dtype == TARDIS_BF16 ? launch_any<__nv_bfloat16, 4>(a, s) : launch_any<float, 4>(a, s);
+  return a.dtype == TARDIS_BF16 ? launch_linear_tc(a, s) : launch_any<float, 4>(a, s);
 }
 
 }  // namespace tardis

@@ -1,0 +1,463 @@
+// The products of linear.cuh for bf16 operands on the 5th-generation tensor cores.
+//
+// The weights are the M side of the MMAs, the rows of x (tokens) the N side: an accumulator has an output channel per TMEM lane and a
+// token per column.  N is chosen for every tile (16 .. 256 in steps of 16, in pairs 32), so a group of any size wastes few columns, and the
+// tokens of a group are cut into tiles of equal width; with the tokens on the M side every group would be padded to 128 rows.  The epilogue
+// comes to 32 neighbouring channels of a token in the 32 lanes of a warp: bias is one value per thread, y and the residual are touched in pieces of 64
+// or 128 bytes.
+//
+// A CTA is persistent: warp 0 stages 128 x 64 (weights) and up to NT x 64 (tokens) boxes with TMA (128-byte swizzle, no multicast), the tokens as boxes
+// of 32 rows or, where the rows of a group are picked by an index array, four rows at a time by their indices (tile::gather4); warp 1 issues the MMAs into
+// one of two accumulators; warps 2 .. 9 run the epilogue of the other.  CTAS = 2: two CTAs share a tile of 256 channels, each with 128 of them and half of
+// the tokens in shared memory (cta_group::2).  SPLIT: the CTAs of a cluster share the channels k of a tile; each hands the others the columns that
+// they finish through their shared memory, and the owner of a column adds the parts in the order of their ranks: no atomics, no scratch, the same bits
+// every time.
+//
+// Every wait on an mbarrier is bounded: when it runs out the CTA stops issuing, fills what it would have written with NaN and ends after its copies have landed.
+#include <cuda.h>
+#include <math_constants.h>
+
+#include "linear.cuh"
+#include "tc.cuh"
+
+namespace tardis {
+namespace linear {
+using namespace tc;
+
+constexpr int BM = 128, BK = 64, BOX = 32;       // channels of a CTA's tile; k per stage; rows per copy of tokens
+constexpr int NTHREADS = 320;
+
+template <int CTAS, int NT, bool SPLIT> struct Cfg {
+  static constexpr int A_BYTES = BM * BK * 2, B_ROWS = NT / CTAS, STAGE_BYTES = A_BYTES + B_ROWS * BK * 2;
+  static constexpr int EXCHANGE = SPLIT ? BM * NT * 4 : 0;
+  static constexpr int NS = (204 * 1024 - EXCHANGE) / STAGE_BYTES;
+  static constexpr int TMEM_COLS = 2 * NT;
+  static constexpr int STEP = 16 * CTAS;                             // of N
+  static constexpr int FIXED = NS * STAGE_BYTES + EXCHANGE + 1024 /* alignment slack */ + 256 /* barriers */;
+};
+
+struct Params {
+  LinearArgs a;
+  int kblocks, splits, band, tokens_fast;
+};
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+               ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_pair(void* dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+               ::"r"(smem_u32(dst)), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+// four rows, one below the other in shared memory (the map's box is one row high)
+__device__ __forceinline__ void tma_gather4(void* dst, const CUtensorMap* map, int x, const int (&r)[4], uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+               ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+__device__ __forceinline__ void tma_gather4_pair(void* dst, const CUtensorMap* map, int x, const int (&r)[4], uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+               ::"r"(smem_u32(dst)), "l"(map), "r"(bar), "r"(x), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+__device__ __forceinline__ uint32_t in_rank(const void* p, int rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  return a;
+}
+// a bounded wait of a whole warp for what other CTAs of the cluster have written
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* b, uint32_t parity) {
+  uint32_t ok = 0;
+  const long long t0 = clock64();
+  do {
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+  } while (!ok && clock64() - t0 <= WAIT_CYCLES);
+  return __all_sync(0xffffffffu, ok != 0);
+}
+
+// One tile as a role sees it.
+struct Tile { int e, o0, first, rows, nt; };     // group, first output, first row, rows, columns of the MMA
+
+template <int ACT> __device__ __forceinline__ float activation(float z) {
+  if (ACT == TARDIS_ACT_GELU_TANH) return gelu_tanh_f32(z);
+  return apply_act(z, ACT);
+}
+
+// Columns c .. c + 31 of a thread's channel: token c + i of the tile is row `row0 + c + i` of y.
+template <int ACT, typename O>
+__device__ __forceinline__ void finish(const LinearArgs& a, const float (&v)[32], long long row, int count, int o, float bias) {
+  O* y = static_cast<O*>(a.y) + row * a.ldy + o;
+  if (a.res) {
+    const O* r = static_cast<const O*>(a.res) + row * a.ldr + o;
+    float old[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) old[i] = i < count ? to_f32(r[i * a.ldr]) : 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (i < count) y[i * a.ldy] = from_f32<O>(activation<ACT>(v[i] + bias) + old[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (i < count) y[i * a.ldy] = from_f32<O>(activation<ACT>(v[i] + bias));
+  }
+}
+template <typename O>
+__device__ __forceinline__ void finish_act(const LinearArgs& a, const float (&v)[32], long long row, int count, int o, float bias) {
+  switch (a.act) {
+    case TARDIS_ACT_GELU_TANH: finish<TARDIS_ACT_GELU_TANH, O>(a, v, row, count, o, bias); break;
+    case TARDIS_ACT_GELU_ERF: finish<TARDIS_ACT_GELU_ERF, O>(a, v, row, count, o, bias); break;
+    case TARDIS_ACT_RELU: finish<TARDIS_ACT_RELU, O>(a, v, row, count, o, bias); break;
+    default: finish<TARDIS_ACT_NONE, O>(a, v, row, count, o, bias);
+  }
+}
+
+template <int CTAS, int NT, bool SPLIT, bool GATHER>
+__global__ void __launch_bounds__(NTHREADS, 1)
+k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ Params p) {
+  using C = Cfg<CTAS, NT, SPLIT>;
+  static_assert(!(SPLIT && CTAS == 2) && C::B_ROWS <= 128, "");
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* const exchange = reinterpret_cast<float*>(smem + C::NS * C::STAGE_BYTES);      // [splits][NT / splits][128]
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE);
+  uint64_t* empty = full + C::NS;
+  uint64_t* accum_full = empty + C::NS;        // [2]
+  uint64_t* accum_empty = accum_full + 2;      // [2]
+  uint64_t* parts_full = accum_empty + 2;      // SPLIT: the other CTAs' parts are here; ... have been taken everywhere
+  uint64_t* parts_empty = parts_full + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(parts_empty + 1);
+  volatile uint32_t* failed = tmem_slot + 1;
+  int* const starts = reinterpret_cast<int*>(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE + 256);   // [groups + 1] first rows (grouped only)
+  int* const firsts = starts + p.a.groups + 1;                                                     // [groups + 1] first tiles
+  static_assert((2 * C::NS + 6) * 8 + 8 <= 256, "");
+
+  const LinearArgs& a = p.a;
+  const int warp = __shfl_sync(0xffffffffu, int(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const int in_cluster = SPLIT ? p.splits : CTAS;
+  const int rank = in_cluster > 1 ? int(cluster_rank()) : 0, first_tile = blockIdx.x / in_cluster, step = gridDim.x / in_cluster;
+  const int mt = (a.o + BM * CTAS - 1) / (BM * CTAS);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::NS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(&accum_full[b], 1); mbar_init(&accum_empty[b], 8 * CTAS); }
+    if (SPLIT) { mbar_init(parts_full, 8 * p.splits); mbar_init(parts_empty, 8 * p.splits); }
+    *failed = 0u;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmW) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmX) : "memory");
+  }
+  if (warp == 1) {
+    if (CTAS == 2) tmem_alloc_pair(tmem_slot, C::TMEM_COLS);
+    else tmem_alloc(tmem_slot, C::TMEM_COLS);
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");             // (x, offsets, ... may come from the launch before)
+  int ntiles;
+  if (a.offsets) {
+    for (int e = threadIdx.x; e <= a.groups; e += NTHREADS) starts[e] = min(max(a.offsets[e], 0), a.n);
+    __syncthreads();
+    if (warp == 2) {                                             // groups disjoint and in order, whatever the array holds; their tiles
+      int end = starts[0], before = 0;
+      __syncwarp();
+      for (int e0 = 0; e0 < a.groups; e0 += 32) {
+        const int e = e0 + lane;
+        int mine = e < a.groups ? max(starts[e + 1], end) : end;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int other = __shfl_up_sync(0xffffffffu, mine, d);
+          if (lane >= d) mine = max(mine, other);
+        }
+        int start = __shfl_up_sync(0xffffffffu, mine, 1);
+        if (lane == 0) start = end;
+        int tiles = (mine - start + NT - 1) / NT * mt;
+        const int own = tiles;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int other = __shfl_up_sync(0xffffffffu, tiles, d);
+          if (lane >= d) tiles += other;
+        }
+        if (e < a.groups) { starts[e + 1] = mine; firsts[e] = before + tiles - own; }
+        end = __shfl_sync(0xffffffffu, mine, 31);
+        before += __shfl_sync(0xffffffffu, tiles, 31);
+      }
+      if (lane == 0) firsts[a.groups] = before;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (in_cluster > 1) cluster_sync();                            // (the other CTAs' barriers are reported to)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (this CTA has its tensor memory)
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  ntiles = a.offsets ? firsts[a.groups] : (a.n + NT - 1) / NT * mt;
+
+  auto decode = [&](int tile) {
+    Tile t;
+    t.e = 0;
+    int group_first = 0, group_rows = a.n, rem = tile;
+    if (a.offsets) {
+      int lo = 0, hi = a.groups;                                 // the last group whose first tile is not behind this one
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (firsts[mid] <= tile) lo = mid;
+        else hi = mid;
+      }
+      t.e = lo;
+      rem = tile - firsts[lo];
+      group_first = starts[lo];
+      group_rows = starts[lo + 1] - group_first;
+    }
+    const int tiles = (group_rows + NT - 1) / NT;
+    const int per = ((group_rows + tiles - 1) / tiles + C::STEP - 1) & ~(C::STEP - 1);         // tokens per tile: as even as the steps allow
+    // raster: bands along one dimension, walked across the other, so that CTAs running at the same time share operands in L2
+    const int F = p.tokens_fast ? tiles : mt, S = p.tokens_fast ? mt : tiles;
+    const int bi = rem / (p.band * S), r2 = rem - bi * (p.band * S);
+    const int w = min(p.band, F - bi * p.band);
+    const int slow = r2 / w, fast = bi * p.band + (r2 - slow * w);
+    const int ni = p.tokens_fast ? fast : slow, mi = p.tokens_fast ? slow : fast;
+    t.o0 = mi * (BM * CTAS) + (CTAS == 2 ? rank * BM : 0);
+    t.first = group_first + ni * per;
+    t.rows = max(0, min(per, group_rows - ni * per));
+    t.nt = max(C::STEP, (t.rows + C::STEP - 1) & ~(C::STEP - 1));
+    return t;
+  };
+  // this CTA's part of the k blocks
+  const int per_split = SPLIT ? (p.kblocks + p.splits - 1) / p.splits : p.kblocks;
+  const int kb_lo = SPLIT ? min(rank * per_split, p.kblocks) : 0, nkb = SPLIT ? min(p.kblocks, kb_lo + per_split) - kb_lo : p.kblocks;
+
+  int issued = 0;
+  if (warp == 0) {
+    // ---------------- copies ----------------
+    int s = 0, parity = 1;
+    for (int tile = first_tile; tile < ntiles; tile += step) {
+      const Tile t = decode(tile);
+      const int half = t.nt / CTAS, row0 = t.first + (CTAS == 2 ? rank * half : 0);      // this CTA's tokens
+      const int boxes = (half + BOX - 1) / BOX;
+      const uint32_t bytes = C::A_BYTES + (GATHER ? half * 128 : boxes * (BOX * 128));
+      int idx[4] = {a.nx, a.nx, a.nx, a.nx};                     // (behind the last row: zeros)
+      if (GATHER) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = row0 + lane * 4 + i;
+          if (r < t.first + t.rows) {
+            const int src = a.rows[r];
+            if (src >= 0 && src < a.nx) idx[i] = src;
+          }
+        }
+      }
+      for (int kb = kb_lo; kb < kb_lo + nkb; ++kb) {
+        if (!mbar_wait_issue(&empty[s], parity, failed)) break;
+        ++issued;
+        uint8_t* const sa = smem + s * C::STAGE_BYTES;
+        uint8_t* const sb = sa + C::A_BYTES;
+        const int kx = kb * BK;
+        if (elect_one()) {
+          if (rank == 0 || CTAS == 1) mbar_expect_tx(&full[s], CTAS * bytes);
+          if (CTAS == 2) tma_load_3d_pair(sa, &tmW, kx, t.o0, t.e, in_rank_0(&full[s]));
+          else tma_load_3d(sa, &tmW, kx, t.o0, t.e, &full[s]);
+          if (!GATHER)
+            for (int i = 0; i < boxes; ++i) {
+              if (CTAS == 2) tma_load_2d_pair(sb + i * (BOX * 128), &tmX, kx, row0 + i * BOX, in_rank_0(&full[s]));
+              else tma_load_2d(sb + i * (BOX * 128), &tmX, kx, row0 + i * BOX, &full[s]);
+            }
+        }
+        if (GATHER) {
+          __syncwarp();                                          // (the bytes are expected before any of them can arrive)
+          if (lane * 4 < half) {
+            if (CTAS == 2) tma_gather4_pair(sb + lane * 512, &tmX, kx, idx, in_rank_0(&full[s]));
+            else tma_gather4(sb + lane * 512, &tmX, kx, idx, &full[s]);
+          }
+          __syncwarp();
+        }
+        if (++s == C::NS) { s = 0; parity ^= 1; }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- MMAs (of a pair: rank 0) ----------------
+    const uint64_t adesc = smem_desc_k_major_sw128(smem_u32(smem)), bdesc = smem_desc_k_major_sw128(smem_u32(smem) + C::A_BYTES);
+    int s = 0, parity = 0;
+    uint32_t use = 0;
+    for (int tile = (CTAS == 1 || rank == 0) && nkb > 0 ? first_tile : ntiles; tile < ntiles; tile += step) {
+      const Tile t = decode(tile);
+      const uint32_t idesc = instr_desc_bf16(BM * CTAS, t.nt);
+      const uint32_t ab = use & 1u;
+      bool ok = mbar_wait_issue(&accum_empty[ab], ((use >> 1) & 1) ^ 1, failed);
+      tc_fence_after();
+      const uint32_t tacc = tmem_base + ab * NT;
+      for (int kb = 0; kb < nkb; ++kb) {
+        ok = mbar_wait_issue(&full[s], parity, failed);
+        tc_fence_after();
+        const uint64_t da = adesc + uint32_t(s * (C::STAGE_BYTES >> 4)), db = bdesc + uint32_t(s * (C::STAGE_BYTES >> 4));
+        if (elect_one() && ok) {
+#pragma unroll
+          for (int k = 0; k < BK / 16; ++k) {
+            if (CTAS == 2) umma_f16_pair(tacc, da + k * 2, db + k * 2, idesc, (kb | k) != 0 ? 1u : 0u);
+            else umma_f16(tacc, da + k * 2, db + k * 2, idesc, (kb | k) != 0 ? 1u : 0u);
+          }
+          if (CTAS == 2) umma_commit_pair(&empty[s]);
+          else umma_commit(&empty[s]);
+        }
+        if (++s == C::NS) { s = 0; parity ^= 1; }
+      }
+      if (elect_one() && ok) {
+        if (CTAS == 2) umma_commit_pair(&accum_full[ab]);
+        else umma_commit(&accum_full[ab]);
+      }
+      ++use;
+    }
+  } else {
+    // ---------------- epilogue: a warp has TMEM lanes 32 (warp % 4) .. + 31 and every other block of 32 columns ----------------
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    uint32_t use = 0;
+    bool ok = true;
+    for (int tile = first_tile; tile < ntiles; tile += step) {
+      const Tile t = decode(tile);
+      const int o = t.o0 + q * 32 + lane;
+      const uint32_t ab = use & 1u;
+      const float bias = a.bias && o < a.o ? a.bias[(long long)(t.e) * a.o + o] : 0.f;
+      if (nkb > 0) ok = ok && mbar_wait_warp(&accum_full[ab], (use >> 1) & 1);
+      if (!ok) *failed = 1u;
+      tc_fence_after();
+      if (!SPLIT) {
+        for (int c = half * 32; c < t.rows; c += 64) {
+          float v[32];
+          tmem_ld32(tmem_base + ab * NT + (uint32_t(q * 32) << 16) + uint32_t(c), v);
+          if (!ok) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = CUDART_NAN_F;
+          }
+          if (o < a.o) {
+            if (a.out_dtype == TARDIS_BF16) finish_act<__nv_bfloat16>(a, v, t.first + c, t.rows - c, o, bias);
+            else finish_act<float>(a, v, t.first + c, t.rows - c, o, bias);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (CTAS == 2) mbar_arrive_cluster(in_rank_0(&accum_empty[ab]));
+          else mbar_arrive(&accum_empty[ab]);
+        }
+      } else {
+        // column c belongs to CTA c % splits, as its column c / splits; the parts of the tile before have been taken by then
+        if (use > 0 && ok) ok = mbar_wait_cluster(parts_empty, (use - 1) & 1);
+        for (int c = half * 32; c < t.rows; c += 64) {
+          float v[32];
+          tmem_ld32(tmem_base + ab * NT + (uint32_t(q * 32) << 16) + uint32_t(c), v);
+          const uint32_t mine = smem_u32(exchange) + uint32_t(rank * (NT / p.splits) * BM + q * 32 + lane) * 4;
+          for (int r = 0; r < p.splits; ++r) {
+            uint32_t to;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(mine), "r"(r));
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if ((c + i) % p.splits == r && c + i < t.rows)
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + uint32_t((c + i) / p.splits * BM * 4)),
+                             "f"(!ok ? CUDART_NAN_F : nkb > 0 ? v[i] : 0.f) : "memory");
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (nkb > 0) mbar_arrive(&accum_empty[ab]);
+          for (int r = 0; r < p.splits; ++r) mbar_arrive_cluster(in_rank(parts_full, r));
+        }
+        ok = mbar_wait_cluster(parts_full, use & 1) && ok;
+        if (!ok) *failed = 1u;
+        for (int i = half; i * p.splits + rank < t.rows; i += 2) {
+          float z = 0.f;
+          for (int r = 0; r < p.splits; ++r) z += exchange[(r * (NT / p.splits) + i) * BM + q * 32 + lane];
+          if (!ok) z = CUDART_NAN_F;
+          if (o < a.o) {
+            const long long row = t.first + i * p.splits + rank;
+            z += bias;
+            z = a.act == TARDIS_ACT_GELU_TANH ? gelu_tanh_f32(z) : apply_act(z, a.act);
+            if (a.res) z += load_out(a.res, row * a.ldr + o, a.out_dtype);
+            store_out(a.y, row * a.ldy + o, a.out_dtype, z);
+          }
+        }
+        __syncwarp();
+        if (lane == 0)
+          for (int r = 0; r < p.splits; ++r) mbar_arrive_cluster(in_rank(parts_empty, r));
+      }
+      ++use;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (CTAS == 2) {
+    // neither ends while the other may still report to it or its MMAs read it; copies of both report to rank 0
+    if (threadIdx.x == 0 && rank == 1 && *failed) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_rank_0(const_cast<uint32_t*>(failed))), "r"(1u) : "memory");
+    cluster_sync();
+    if (rank == 0 && warp == 0 && *failed) land_copies<C::NS>(full, issued);
+    if (warp == 1) tmem_dealloc_pair(tmem_base, C::TMEM_COLS);
+    cluster_sync();
+  } else {
+    if (warp == 0 && *failed) land_copies<C::NS>(full, issued);
+    if (warp == 1) tmem_dealloc(tmem_base, C::TMEM_COLS);
+    if (SPLIT) cluster_sync();
+  }
+}
+
+// ---- host side ------------------------------------------------------------------------------------------
+static bool make_weight_map(CUtensorMap* map, const LinearArgs& a) {
+  return make_map_3d(map, a.W, a.o, a.groups, a.k, a.ldw, a.groups > 1 ? a.stride_w : a.ldw, BM);
+}
+
+template <int CTAS, int NT, bool SPLIT, bool GATHER>
+static tardis_status_t launch(const LinearArgs& a, int splits, int dev, int sms, cudaStream_t s) {
+  using C = Cfg<CTAS, NT, SPLIT>;
+  CUtensorMap w, x;
+  if (!make_weight_map(&w, a) || !make_map(&x, a.x, a.nx, a.k, a.ldx, GATHER ? 1 : BOX)) return TARDIS_ERR_INVALID_ARG;
+  Params p;
+  p.a = a; p.kblocks = (a.k + BK - 1) / BK; p.splits = splits;
+  const long long mt = (a.o + BM * CTAS - 1) / (BM * CTAS), nt = (a.n + NT - 1) / NT;
+  p.tokens_fast = nt <= mt ? 1 : 0;
+  p.band = 8;
+  const int smem = C::FIXED + (a.offsets ? 8 * (a.groups + 1) : 0);
+  static thread_local int room_on = -1;               // the device on which this thread last gave the kernel its shared memory
+  if (dev != room_on) {
+    TARDIS_CUDA_TRY(cudaFuncSetAttribute(k_linear_tc<CTAS, NT, SPLIT, GATHER>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::FIXED + 8 * (kMaxExperts + 1)));
+    room_on = dev;
+  }
+  long long tiles = (nt + (a.offsets ? (a.groups < a.n ? a.groups : a.n) : 0)) * mt;     // at most
+  const int in_cluster = SPLIT ? splits : CTAS;
+  const long long at_once = sms / in_cluster;
+  if (tiles > at_once) tiles = at_once;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(tiles * in_cluster)); cfg.blockDim = dim3(NTHREADS); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = in_cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = in_cluster > 1 ? 2 : 1;
+  TARDIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_linear_tc<CTAS, NT, SPLIT, GATHER>, w, x, p));
+  return TARDIS_OK;
+}
+
+template <int CTAS, int NT, bool SPLIT>
+static tardis_status_t launch_rows(const LinearArgs& a, int splits, int dev, int sms, cudaStream_t s) {
+  return a.rows ? launch<CTAS, NT, SPLIT, true>(a, splits, dev, sms, s) : launch<CTAS, NT, SPLIT, false>(a, splits, dev, sms, s);
+}
+
+}  // namespace linear
+
+tardis_status_t launch_linear_tc(const LinearArgs& a, cudaStream_t s) {
+  using namespace linear;
+  if (!tensor_maps_available()) return TARDIS_ERR_UNSUPPORTED;
+  int dev = 0, sms = 0;
+  TARDIS_CUDA_TRY(cudaGetDevice(&dev));
+  TARDIS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  const long long groups = a.groups, per_group = (a.n + groups - 1) / groups;
+  const long long pair_tiles = ((a.o + 255) / 256) * (a.offsets ? groups * ((per_group + 255) / 256) : (a.n + 255) / 256);
+  if (per_group > 128 && pair_tiles * 2 * 10 >= sms * 7) return launch_rows<2, 256, false>(a, 1, dev, sms, s);
+  const long long tiles = ((a.o + 127) / 128) * (a.offsets ? groups : 1);
+  const int kblocks = (a.k + BK - 1) / BK;
+  if (per_group <= 64) {
+    int splits = 1;
+    while (splits < 8 && tiles * splits * 2 <= sms && kblocks / (splits * 2) >= 4) splits *= 2;
+    return splits > 1 ? launch_rows<1, 64, true>(a, splits, dev, sms, s) : launch_rows<1, 64, false>(a, 1, dev, sms, s);
+  }
+  const long long tiles2 = tiles * ((per_group + 127) / 128);
+  int splits = 1;
+  while (splits < 8 && tiles2 * splits * 2 <= sms && kblocks / (splits * 2) >= 4) splits *= 2;
+  return splits > 1 ? launch_rows<1, 128, true>(a, splits, dev, sms, s) : launch_rows<1, 128, false>(a, 1, dev, sms, s);
+}
+
+}  // namespace tardis

@@ -200,7 +200,9 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
 // Host: tensor map of a bf16 matrix [rows, K] row-major with leading dimension ld; box = 64 channels x box_rows rows, 128-byte
 // swizzle; elements outside the matrix read as zero.  False where the driver has no tensor-map support or refuses the matrix.
 bool tensor_maps_available();
-bool make_map(CUtensorMap* map, const void* base, int rows, int K, int ld, int box_rows);
+bool make_map(CUtensorMap* map, const void* base, int rows, int K, long long ld, int box_rows);
+// the same of `count` such matrices `stride` elements apart (box: one of them)
+bool make_map_3d(CUtensorMap* map, const void* base, int rows, int count, int K, long long ld, long long stride, int box_rows);
 
 }  // namespace tc
 }  // namespace tardis
