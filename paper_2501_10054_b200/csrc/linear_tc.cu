@@ -25,11 +25,12 @@ namespace linear {
 using namespace tc;
 
 constexpr int BM = 128, BK = 64, BOX = 32;       // channels of a CTA's tile; k per stage; rows per copy of tokens
-constexpr int NTHREADS = 320;
+constexpr int NTHREADS = 320, GATHER_WARPS = 4;
 
-template <int CTAS, int NT, bool SPLIT> struct Cfg {
+template <int CTAS, int NT, int SPLITS> struct Cfg {
   static constexpr int A_BYTES = BM * BK * 2, B_ROWS = NT / CTAS, STAGE_BYTES = A_BYTES + B_ROWS * BK * 2;
-  static constexpr int EXCHANGE = SPLIT ? BM * NT * 4 : 0;
+  static constexpr int SHARE = (31 + SPLITS) / SPLITS;               // columns of a block of 32 that a CTA of the cluster finishes, at most
+  static constexpr int EXCHANGE = SPLITS > 1 ? SPLITS * (NT / 32 * SHARE) * BM * 4 : 0;
   static constexpr int NS = (204 * 1024 - EXCHANGE) / STAGE_BYTES;
   static constexpr int TMEM_COLS = 2 * NT;
   static constexpr int STEP = 16 * CTAS;                             // of N
@@ -38,7 +39,7 @@ template <int CTAS, int NT, bool SPLIT> struct Cfg {
 
 struct Params {
   LinearArgs a;
-  int kblocks, splits, band, tokens_fast;
+  int kblocks, band, tokens_fast;
 };
 
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
@@ -110,14 +111,15 @@ __device__ __forceinline__ void finish_act(const LinearArgs& a, const float (&v)
   }
 }
 
-template <int CTAS, int NT, bool SPLIT, bool GATHER>
-__global__ void __launch_bounds__(NTHREADS, 1)
+template <int CTAS, int NT, int SPLITS, bool GATHER>
+__global__ void __launch_bounds__(NTHREADS + (GATHER ? 32 * GATHER_WARPS : 0), 1)
 k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ Params p) {
-  using C = Cfg<CTAS, NT, SPLIT>;
+  using C = Cfg<CTAS, NT, SPLITS>;
+  constexpr bool SPLIT = SPLITS > 1;
   static_assert(!(SPLIT && CTAS == 2) && C::B_ROWS <= 128, "");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* const exchange = reinterpret_cast<float*>(smem + C::NS * C::STAGE_BYTES);      // [splits][NT / splits][128]
+  float* const exchange = reinterpret_cast<float*>(smem + C::NS * C::STAGE_BYTES);      // [SPLITS][NT / 32 * SHARE][128]
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE);
   uint64_t* empty = full + C::NS;
   uint64_t* accum_full = empty + C::NS;        // [2]
@@ -132,13 +134,13 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
 
   const LinearArgs& a = p.a;
   const int warp = __shfl_sync(0xffffffffu, int(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-  const int in_cluster = SPLIT ? p.splits : CTAS;
+  constexpr int in_cluster = SPLITS * CTAS;
   const int rank = in_cluster > 1 ? int(cluster_rank()) : 0, first_tile = blockIdx.x / in_cluster, step = gridDim.x / in_cluster;
   const int mt = (a.o + BM * CTAS - 1) / (BM * CTAS);
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::NS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(&accum_full[b], 1); mbar_init(&accum_empty[b], 8 * CTAS); }
-    if (SPLIT) { mbar_init(parts_full, 8 * p.splits); mbar_init(parts_empty, 8 * p.splits); }
+    if (SPLIT) { mbar_init(parts_full, 8 * SPLITS); mbar_init(parts_empty, 8 * SPLITS); }
     *failed = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tmW) : "memory");
@@ -151,7 +153,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   asm volatile("griddepcontrol.wait;" ::: "memory");             // (x, offsets, ... may come from the launch before)
   int ntiles;
   if (a.offsets) {
-    for (int e = threadIdx.x; e <= a.groups; e += NTHREADS) starts[e] = min(max(a.offsets[e], 0), a.n);
+    for (int e = threadIdx.x; e <= a.groups; e += blockDim.x) starts[e] = min(max(a.offsets[e], 0), a.n);
     __syncthreads();
     if (warp == 2) {                                             // groups disjoint and in order, whatever the array holds; their tiles
       int end = starts[0], before = 0;
@@ -219,7 +221,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     return t;
   };
   // this CTA's part of the k blocks
-  const int per_split = SPLIT ? (p.kblocks + p.splits - 1) / p.splits : p.kblocks;
+  const int per_split = SPLIT ? (p.kblocks + SPLITS - 1) / SPLITS : p.kblocks;
   const int kb_lo = SPLIT ? min(rank * per_split, p.kblocks) : 0, nkb = SPLIT ? min(p.kblocks, kb_lo + per_split) - kb_lo : p.kblocks;
 
   int issued = 0;
@@ -230,18 +232,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       const Tile t = decode(tile);
       const int half = t.nt / CTAS, row0 = t.first + (CTAS == 2 ? rank * half : 0);      // this CTA's tokens
       const int boxes = (half + BOX - 1) / BOX;
-      const uint32_t bytes = C::A_BYTES + (GATHER ? half * 128 : boxes * (BOX * 128));
-      int idx[4] = {a.nx, a.nx, a.nx, a.nx};                     // (behind the last row: zeros)
-      if (GATHER) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = row0 + lane * 4 + i;
-          if (r < t.first + t.rows) {
-            const int src = a.rows[r];
-            if (src >= 0 && src < a.nx) idx[i] = src;
-          }
-        }
-      }
+      const uint32_t bytes = C::A_BYTES + (GATHER ? half * 128 : boxes * (BOX * 128));       // (of the gathered rows too)
       for (int kb = kb_lo; kb < kb_lo + nkb; ++kb) {
         if (!mbar_wait_issue(&empty[s], parity, failed)) break;
         ++issued;
@@ -257,14 +248,6 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
               if (CTAS == 2) tma_load_2d_pair(sb + i * (BOX * 128), &tmX, kx, row0 + i * BOX, in_rank_0(&full[s]));
               else tma_load_2d(sb + i * (BOX * 128), &tmX, kx, row0 + i * BOX, &full[s]);
             }
-        }
-        if (GATHER) {
-          __syncwarp();                                          // (the bytes are expected before any of them can arrive)
-          if (lane * 4 < half) {
-            if (CTAS == 2) tma_gather4_pair(sb + lane * 512, &tmX, kx, idx, in_rank_0(&full[s]));
-            else tma_gather4(sb + lane * 512, &tmX, kx, idx, &full[s]);
-          }
-          __syncwarp();
         }
         if (++s == C::NS) { s = 0; parity ^= 1; }
       }
@@ -302,6 +285,38 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       }
       ++use;
     }
+  } else if (GATHER && warp >= NTHREADS / 32) {
+    // ---------------- rows of x by their indices ----------------
+    // Each of four warps has a quarter of this CTA's rows, their indices in registers that all lanes hold alike, and copies them four at a time.
+    constexpr int QUADS = C::B_ROWS / (4 * GATHER_WARPS);
+    const int w = warp - NTHREADS / 32;
+    int s = 0, parity = 1;
+    for (int tile = first_tile; tile < ntiles; tile += step) {
+      const Tile t = decode(tile);
+      const int half = t.nt / CTAS, row0 = t.first + (CTAS == 2 ? rank * half : 0);
+      int idx[QUADS][4];
+#pragma unroll
+      for (int j = 0; j < QUADS; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = row0 + (w + j * GATHER_WARPS) * 4 + i;
+          const int at = r < t.first + t.rows ? a.rows[r] : -1;
+          idx[j][i] = at >= 0 && at < a.nx ? at : a.nx;          // (behind the last row: zeros)
+        }
+      for (int kb = kb_lo; kb < kb_lo + nkb; ++kb) {
+        if (!mbar_wait_issue(&empty[s], parity, failed)) break;
+        if (elect_one()) {
+          uint8_t* const sb = smem + s * C::STAGE_BYTES + C::A_BYTES + w * 512;
+#pragma unroll
+          for (int j = 0; j < QUADS; ++j)
+            if ((w + j * GATHER_WARPS) * 4 < half) {
+              if (CTAS == 2) tma_gather4_pair(sb + j * (GATHER_WARPS * 512), &tmX, kb * BK, idx[j], in_rank_0(&full[s]));
+              else tma_gather4(sb + j * (GATHER_WARPS * 512), &tmX, kb * BK, idx[j], &full[s]);
+            }
+        }
+        if (++s == C::NS) { s = 0; parity ^= 1; }
+      }
+    }
   } else {
     // ---------------- epilogue: a warp has TMEM lanes 32 (warp % 4) .. + 31 and every other block of 32 columns ----------------
     const int q = warp & 3, half = (warp - 2) >> 2;
@@ -335,45 +350,56 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
           else mbar_arrive(&accum_empty[ab]);
         }
       } else {
-        // column c belongs to CTA c % splits, as its column c / splits; the parts of the tile before have been taken by then
+        // of every block of 32 columns, column i belongs to CTA i % SPLITS; the parts of the tile before have been taken by then
         if (use > 0 && ok) ok = mbar_wait_cluster(parts_empty, (use - 1) & 1);
+        constexpr int SHARE = C::SHARE, WIDTH = NT / 32 * SHARE;
+        uint32_t to[SPLITS];
+#pragma unroll
+        for (int r = 0; r < SPLITS; ++r) to[r] = in_rank(exchange + rank * WIDTH * BM + q * 32 + lane, r);
         for (int c = half * 32; c < t.rows; c += 64) {
           float v[32];
           tmem_ld32(tmem_base + ab * NT + (uint32_t(q * 32) << 16) + uint32_t(c), v);
-          const uint32_t mine = smem_u32(exchange) + uint32_t(rank * (NT / p.splits) * BM + q * 32 + lane) * 4;
-          for (int r = 0; r < p.splits; ++r) {
-            uint32_t to;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(mine), "r"(r));
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if ((c + i) % p.splits == r && c + i < t.rows)
-                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + uint32_t((c + i) / p.splits * BM * 4)),
-                             "f"(!ok ? CUDART_NAN_F : nkb > 0 ? v[i] : 0.f) : "memory");
-          }
+          for (int i = 0; i < 32; ++i)
+            if (c + i < t.rows)
+              asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to[i % SPLITS] + uint32_t(c / 32 * SHARE + i / SPLITS) * (BM * 4)),
+                           "f"(!ok ? CUDART_NAN_F : nkb > 0 ? v[i] : 0.f) : "memory");
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
           if (nkb > 0) mbar_arrive(&accum_empty[ab]);
-          for (int r = 0; r < p.splits; ++r) mbar_arrive_cluster(in_rank(parts_full, r));
+#pragma unroll
+          for (int r = 0; r < SPLITS; ++r) mbar_arrive_cluster(in_rank(parts_full, r));
         }
         ok = mbar_wait_cluster(parts_full, use & 1) && ok;
         if (!ok) *failed = 1u;
-        for (int i = half; i * p.splits + rank < t.rows; i += 2) {
-          float z = 0.f;
-          for (int r = 0; r < p.splits; ++r) z += exchange[(r * (NT / p.splits) + i) * BM + q * 32 + lane];
-          if (!ok) z = CUDART_NAN_F;
-          if (o < a.o) {
-            const long long row = t.first + i * p.splits + rank;
+        // this CTA's columns, eight at a time (the loads of eight residuals at once)
+        for (int w0 = half * 8; w0 < WIDTH; w0 += 16) {
+          float old[8];
+          bool mine[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int w = w0 + j, i = w % SHARE * SPLITS + rank, c = w / SHARE * 32 + i;
+            mine[j] = w < WIDTH && i < 32 && c < t.rows && o < a.o;
+            old[j] = mine[j] && a.res ? load_out(a.res, (t.first + c) * a.ldr + o, a.out_dtype) : 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            if (!mine[j]) continue;
+            const int w = w0 + j, c = w / SHARE * 32 + w % SHARE * SPLITS + rank;
+            float z = 0.f;
+#pragma unroll
+            for (int r = 0; r < SPLITS; ++r) z += exchange[(r * WIDTH + w) * BM + q * 32 + lane];
             z += bias;
             z = a.act == TARDIS_ACT_GELU_TANH ? gelu_tanh_f32(z) : apply_act(z, a.act);
-            if (a.res) z += load_out(a.res, row * a.ldr + o, a.out_dtype);
-            store_out(a.y, row * a.ldy + o, a.out_dtype, z);
+            if (a.res) z += old[j];
+            store_out(a.y, (t.first + c) * a.ldy + o, a.out_dtype, ok ? z : CUDART_NAN_F);
           }
         }
         __syncwarp();
         if (lane == 0)
-          for (int r = 0; r < p.splits; ++r) mbar_arrive_cluster(in_rank(parts_empty, r));
+          for (int r = 0; r < SPLITS; ++r) mbar_arrive_cluster(in_rank(parts_empty, r));
       }
       ++use;
     }
@@ -399,41 +425,50 @@ static bool make_weight_map(CUtensorMap* map, const LinearArgs& a) {
   return make_map_3d(map, a.W, a.o, a.groups, a.k, a.ldw, a.groups > 1 ? a.stride_w : a.ldw, BM);
 }
 
-template <int CTAS, int NT, bool SPLIT, bool GATHER>
-static tardis_status_t launch(const LinearArgs& a, int splits, int dev, int sms, cudaStream_t s) {
-  using C = Cfg<CTAS, NT, SPLIT>;
+template <int CTAS, int NT, int SPLITS, bool GATHER>
+static tardis_status_t launch(const LinearArgs& a, int dev, int sms, cudaStream_t s) {
+  using C = Cfg<CTAS, NT, SPLITS>;
   CUtensorMap w, x;
   if (!make_weight_map(&w, a) || !make_map(&x, a.x, a.nx, a.k, a.ldx, GATHER ? 1 : BOX)) return TARDIS_ERR_INVALID_ARG;
   Params p;
-  p.a = a; p.kblocks = (a.k + BK - 1) / BK; p.splits = splits;
+  p.a = a; p.kblocks = (a.k + BK - 1) / BK;
   const long long mt = (a.o + BM * CTAS - 1) / (BM * CTAS), nt = (a.n + NT - 1) / NT;
   p.tokens_fast = nt <= mt ? 1 : 0;
   p.band = 8;
   const int smem = C::FIXED + (a.offsets ? 8 * (a.groups + 1) : 0);
   static thread_local int room_on = -1;               // the device on which this thread last gave the kernel its shared memory
   if (dev != room_on) {
-    TARDIS_CUDA_TRY(cudaFuncSetAttribute(k_linear_tc<CTAS, NT, SPLIT, GATHER>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::FIXED + 8 * (kMaxExperts + 1)));
+    TARDIS_CUDA_TRY(cudaFuncSetAttribute(k_linear_tc<CTAS, NT, SPLITS, GATHER>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::FIXED + 8 * (kMaxExperts + 1)));
     room_on = dev;
   }
   long long tiles = (nt + (a.offsets ? (a.groups < a.n ? a.groups : a.n) : 0)) * mt;     // at most
-  const int in_cluster = SPLIT ? splits : CTAS;
+  constexpr int in_cluster = SPLITS * CTAS;
   const long long at_once = sms / in_cluster;
   if (tiles > at_once) tiles = at_once;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(tiles * in_cluster)); cfg.blockDim = dim3(NTHREADS); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+  cfg.gridDim = dim3(unsigned(tiles * in_cluster)); cfg.blockDim = dim3(NTHREADS + (GATHER ? 32 * GATHER_WARPS : 0)); cfg.dynamicSmemBytes = smem; cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = in_cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = in_cluster > 1 ? 2 : 1;
-  TARDIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_linear_tc<CTAS, NT, SPLIT, GATHER>, w, x, p));
+  TARDIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_linear_tc<CTAS, NT, SPLITS, GATHER>, w, x, p));
   return TARDIS_OK;
 }
 
-template <int CTAS, int NT, bool SPLIT>
-static tardis_status_t launch_rows(const LinearArgs& a, int splits, int dev, int sms, cudaStream_t s) {
-  return a.rows ? launch<CTAS, NT, SPLIT, true>(a, splits, dev, sms, s) : launch<CTAS, NT, SPLIT, false>(a, splits, dev, sms, s);
+template <int CTAS, int NT, int SPLITS>
+static tardis_status_t launch_rows(const LinearArgs& a, int dev, int sms, cudaStream_t s) {
+  return a.rows ? launch<CTAS, NT, SPLITS, true>(a, dev, sms, s) : launch<CTAS, NT, SPLITS, false>(a, dev, sms, s);
+}
+template <int NT>
+static tardis_status_t launch_splits(const LinearArgs& a, int splits, int dev, int sms, cudaStream_t s) {
+  switch (splits) {
+    case 2: return launch_rows<1, NT, 2>(a, dev, sms, s);
+    case 3: return launch_rows<1, NT, 3>(a, dev, sms, s);
+    case 4: return launch_rows<1, NT, 4>(a, dev, sms, s);
+  }
+  return launch_rows<1, NT, 1>(a, dev, sms, s);
 }
 
 }  // namespace linear
@@ -446,18 +481,14 @@ tardis_status_t launch_linear_tc(const LinearArgs& a, cudaStream_t s) {
   TARDIS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   const long long groups = a.groups, per_group = (a.n + groups - 1) / groups;
   const long long pair_tiles = ((a.o + 255) / 256) * (a.offsets ? groups * ((per_group + 255) / 256) : (a.n + 255) / 256);
-  if (per_group > 128 && pair_tiles * 2 * 10 >= sms * 7) return launch_rows<2, 256, false>(a, 1, dev, sms, s);
+  if (per_group > 128 && pair_tiles * 2 * 10 >= sms * 7) return launch_rows<2, 256, 1>(a, dev, sms, s);
   const long long tiles = ((a.o + 127) / 128) * (a.offsets ? groups : 1);
   const int kblocks = (a.k + BK - 1) / BK;
-  if (per_group <= 64) {
-    int splits = 1;
-    while (splits < 8 && tiles * splits * 2 <= sms && kblocks / (splits * 2) >= 4) splits *= 2;
-    return splits > 1 ? launch_rows<1, 64, true>(a, splits, dev, sms, s) : launch_rows<1, 64, false>(a, 1, dev, sms, s);
-  }
-  const long long tiles2 = tiles * ((per_group + 127) / 128);
-  int splits = 1;
-  while (splits < 8 && tiles2 * splits * 2 <= sms && kblocks / (splits * 2) >= 4) splits *= 2;
-  return splits > 1 ? launch_rows<1, 128, true>(a, splits, dev, sms, s) : launch_rows<1, 128, false>(a, 1, dev, sms, s);
+  const bool narrow = per_group <= 64;
+  const long long all = narrow ? tiles : tiles * ((per_group + 127) / 128);
+  int splits = 4;
+  while (splits > 1 && (all * splits > (splits == 4 ? 132 : sms) || kblocks / splits < 4)) --splits;
+  return narrow ? launch_splits<64>(a, splits, dev, sms, s) : launch_splits<128>(a, splits, dev, sms, s);
 }
 
 }  // namespace tardis
