@@ -194,7 +194,7 @@ tardis_status_t tardis_gemm_bf16(int32_t M, int32_t N, int32_t K, const void* A,
  * y may be residual (in place, with ldr = ldy) and overlaps none of the other inputs.  n = 0 does nothing.  Asynchronous
  * on `stream`; allocates nothing; nothing is kept; the same bits from run to run.  (Should a wait inside the tensor-core
  * kernel run out, which no valid call makes happen, the tile concerned is filled with NaN.)
- * Errors: INVALID_ARG, UNSUPPORTED (driver without tensor-map support; more than 4194240 rows of fp32), CUDA. */
+ * Errors: INVALID_ARG, UNSUPPORTED (driver without tensor-map support; more than some 4 million rows of fp32), CUDA. */
 #define TARDIS_ACT_NONE (-1)
 typedef struct {
   int64_t n;                  /* rows of x and y (tokens); below 2^31 */

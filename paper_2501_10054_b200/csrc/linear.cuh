@@ -80,6 +80,50 @@ __device__ __forceinline__ GroupTile find_group_tile(const int* offsets, int gro
   return t;
 }
 
+// The same as a table in shared memory, made by all threads of a CTA (callers synchronise afterwards): starts[e], where group e begins (its end is
+// starts[e + 1]), and firsts[e], the tiles in front of it when every `per` rows make `each` tiles.
+__device__ __forceinline__ void build_groups(const int* offsets, int groups, int n, int per, int each, int* starts, int* firsts) {
+  for (int e = threadIdx.x; e <= groups; e += blockDim.x) starts[e] = min(max(offsets[e], 0), n);
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  const int lane = threadIdx.x;
+  int end = starts[0], before = 0;
+  __syncwarp();
+  for (int e0 = 0; e0 < groups; e0 += 32) {
+    const int e = e0 + lane;
+    int mine = e < groups ? max(starts[e + 1], end) : end;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int other = __shfl_up_sync(0xffffffffu, mine, d);
+      if (lane >= d) mine = max(mine, other);
+    }
+    int start = __shfl_up_sync(0xffffffffu, mine, 1);
+    if (lane == 0) start = end;
+    const int own = (mine - start + per - 1) / per * each;
+    int tiles = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int other = __shfl_up_sync(0xffffffffu, tiles, d);
+      if (lane >= d) tiles += other;
+    }
+    if (e < groups) { starts[e + 1] = mine; firsts[e] = before + tiles - own; }
+    end = __shfl_sync(0xffffffffu, mine, 31);
+    before += __shfl_sync(0xffffffffu, tiles, 31);
+    __syncwarp();
+  }
+  if (lane == 0) firsts[groups] = before;
+}
+// the group that has tile `tile` (below firsts[groups])
+__device__ __forceinline__ int group_of(const int* firsts, int groups, int tile) {
+  int lo = 0, hi = groups;                                   // the last group whose first tile is not behind this one
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (firsts[mid] <= tile) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
 __device__ __forceinline__ float apply_act(float z, int act) {
   if (act == TARDIS_ACT_NONE) return z;
   if (act == TARDIS_ACT_RELU) return z < 0.f ? 0.f : z;              // (of -inf 0, of NaN NaN)

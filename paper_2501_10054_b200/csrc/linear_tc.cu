@@ -152,36 +152,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");             // (x, offsets, ... may come from the launch before)
   int ntiles;
-  if (a.offsets) {
-    for (int e = threadIdx.x; e <= a.groups; e += blockDim.x) starts[e] = min(max(a.offsets[e], 0), a.n);
-    __syncthreads();
-    if (warp == 2) {                                             // groups disjoint and in order, whatever the array holds; their tiles
-      int end = starts[0], before = 0;
-      __syncwarp();
-      for (int e0 = 0; e0 < a.groups; e0 += 32) {
-        const int e = e0 + lane;
-        int mine = e < a.groups ? max(starts[e + 1], end) : end;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const int other = __shfl_up_sync(0xffffffffu, mine, d);
-          if (lane >= d) mine = max(mine, other);
-        }
-        int start = __shfl_up_sync(0xffffffffu, mine, 1);
-        if (lane == 0) start = end;
-        int tiles = (mine - start + NT - 1) / NT * mt;
-        const int own = tiles;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const int other = __shfl_up_sync(0xffffffffu, tiles, d);
-          if (lane >= d) tiles += other;
-        }
-        if (e < a.groups) { starts[e + 1] = mine; firsts[e] = before + tiles - own; }
-        end = __shfl_sync(0xffffffffu, mine, 31);
-        before += __shfl_sync(0xffffffffu, tiles, 31);
-      }
-      if (lane == 0) firsts[a.groups] = before;
-    }
-  }
+  if (a.offsets) build_groups(a.offsets, a.groups, a.n, NT, mt, starts, firsts);
   tc_fence_before();
   __syncthreads();
   if (in_cluster > 1) cluster_sync();                            // (the other CTAs' barriers are reported to)
@@ -195,16 +166,10 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     t.e = 0;
     int group_first = 0, group_rows = a.n, rem = tile;
     if (a.offsets) {
-      int lo = 0, hi = a.groups;                                 // the last group whose first tile is not behind this one
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (firsts[mid] <= tile) lo = mid;
-        else hi = mid;
-      }
-      t.e = lo;
-      rem = tile - firsts[lo];
-      group_first = starts[lo];
-      group_rows = starts[lo + 1] - group_first;
+      t.e = group_of(firsts, a.groups, tile);
+      rem = tile - firsts[t.e];
+      group_first = starts[t.e];
+      group_rows = starts[t.e + 1] - group_first;
     }
     const int tiles = (group_rows + NT - 1) / NT;
     const int per = ((group_rows + tiles - 1) / tiles + C::STEP - 1) & ~(C::STEP - 1);         // tokens per tile: as even as the steps allow
