@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -194,26 +195,38 @@ def tardis_gemm_bf16(A: torch.Tensor, B: torch.Tensor, C: torch.Tensor, stream=N
     return C
 
 
-def _rows_of(t: torch.Tensor, name: str, dtype, shape, device):
+# The descriptors of tardis_linear and tardis_grouped_linear as packed bytes (native alignment, as LinearDesc and GroupedDesc): a call that is over in
+# a few microseconds on the device should not take longer to describe.
+_PACK_LINEAR = struct.Struct("@qiiiiiPqPqPPqPq").pack
+_PACK_GROUPED = struct.Struct("@qiiiiiiPqqPqqPPPPqPqqiPPPN").pack
+
+
+def _current(x: torch.Tensor) -> int:
+    """The index of x's device, which has to be the current one: that is where the launch goes."""
+    index = x.get_device()
+    if index < 0 or index != torch.cuda.current_device():
+        raise TardisError(1, "tensors must lie on the current CUDA device")
+    return index
+
+
+def _matrix(t: torch.Tensor, name: str, dtype, rows: int, cols: int, index: int):
     """(data pointer, leading dimension) of a matrix with unit inner stride."""
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise TardisError(1, "%s must be a %s tensor of shape %s on %s with unit inner stride" % (name, dtype, shape, device))
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    shape, (ld, unit) = t.shape, t.stride()
+    if t.dtype is not dtype or shape[0] != rows or shape[1] != cols or t.get_device() != index or (unit != 1 and cols > 1):
+        raise TardisError(1, "%s must be a %s matrix of %d x %d on the same device with unit inner stride" % (name, dtype, rows, cols))
+    return t.data_ptr(), ld if rows > 1 else cols
 
 
-def _vector(t: Optional[torch.Tensor], name: str, dtype, shape, device) -> Optional[int]:
+def _vector(t: Optional[torch.Tensor], name: str, dtype, shape, index: int) -> int:
     if t is None:
-        return None
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
-        raise TardisError(1, "%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, shape, device))
+        return 0
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise TardisError(1, "%s must be a contiguous %s tensor of shape %s on the same device" % (name, dtype, shape))
     return t.data_ptr()
 
 
-def _operand_device(x: torch.Tensor):
-    """x's device, which has to be the current one: that is where the launch goes."""
-    if not x.is_cuda or x.device.index != torch.cuda.current_device():
-        raise TardisError(1, "tensors must lie on the current CUDA device")
-    return x.device
+def _raw_stream(stream, index: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
 
 
 def tardis_linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = TARDIS_ACT_NONE,
@@ -221,58 +234,63 @@ def tardis_linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor]
     """y = act(x W^T + bias) + residual in one launch (see tardis_linear in tardis.h): x [n, k], W [o, k] float32 or bfloat16
     with unit inner stride, bias [o] float32, residual and y [n, o] in out_dtype (x's dtype, or float32).  Returns y (`out`
     when given; it may be the residual)."""
-    dev = _operand_device(x)
     if x.dim() != 2 or W.dim() != 2 or W.shape[1] != x.shape[1]:
         raise TardisError(1, "x must be [n, k] and W [o, k]")
+    index, dtype = _current(x), x.dtype
     (n, k), o = x.shape, W.shape[0]
     if out_dtype is None:
-        out_dtype = x.dtype if out is None else out.dtype
+        out_dtype = dtype if out is None else out.dtype
+    code, out_code = _dtype_code(dtype), _dtype_code(out_dtype)
     if out is None:
-        out = torch.empty(n, o, dtype=out_dtype, device=dev)
-    px, ldx = _rows_of(x, "x", x.dtype, (n, k), dev)
-    pw, ldw = _rows_of(W, "W", x.dtype, (o, k), dev)
-    py, ldy = _rows_of(out, "out", out_dtype, (n, o), dev)
-    pr, ldr = _rows_of(residual, "residual", out_dtype, (n, o), dev) if residual is not None else (None, 0)
-    desc = LinearDesc(n, k, o, _dtype_code(x.dtype), _dtype_code(out_dtype), act, px, ldx, pw, ldw,
-                      _vector(bias, "bias", torch.float32, (o,), dev), pr, ldr, py, ldy)
-    _check(load_library().tardis_linear(ctypes.byref(desc), _stream(stream)), "tardis_linear")
+        out = x.new_empty((n, o), dtype=out_dtype)
+    px, ldx = _matrix(x, "x", dtype, n, k, index)
+    pw, ldw = _matrix(W, "W", dtype, o, k, index)
+    py, ldy = _matrix(out, "out", out_dtype, n, o, index)
+    pr, ldr = _matrix(residual, "residual", out_dtype, n, o, index) if residual is not None else (0, 0)
+    desc = _PACK_LINEAR(n, k, o, code, out_code, act, px, ldx, pw, ldw, _vector(bias, "bias", torch.float32, (o,), index), pr, ldr, py, ldy)
+    status = load_library().tardis_linear(desc, _raw_stream(stream, index))
+    if status != TARDIS_OK:
+        _check(status, "tardis_linear")
     return out
 
 
 def _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, back, work, stream, what):
-    dev = _operand_device(x)
     if x.dim() != 2 or W.dim() != 3 or W.shape[2] != x.shape[1]:
         raise TardisError(1, "x must be [n, k] and W [experts, o, k]")
+    index, dtype, i32 = _current(x), x.dtype, torch.int32
     (nx, k), (experts, o, _) = x.shape, W.shape
     n = nx if rows is None else rows.numel()
     if out_dtype is None:
-        out_dtype = x.dtype if out is None else out.dtype
-    slots, weights = back if back is not None else (None, None)
-    if slots is not None and slots.dim() != 2:
-        raise TardisError(1, "slots must be [tokens, top_k]")
-    tokens, top_k = slots.shape if slots is not None else (0, 0)
-    n_out = n if slots is None else tokens
-    if out is None:
-        out = torch.empty(n_out, o, dtype=out_dtype, device=dev)
-    room = 0
-    if slots is not None:
-        room = 4 * n * o
+        out_dtype = dtype if out is None else out.dtype
+    code, out_code = _dtype_code(dtype), _dtype_code(out_dtype)
+    tokens = top_k = room = ps = pc = pwork = 0
+    n_out = n
+    if back is not None:
+        slots, weights = back
+        if slots.dim() != 2:
+            raise TardisError(1, "slots must be [tokens, top_k]")
+        tokens, top_k = slots.shape
+        ps, pc = _vector(slots, "slots", i32, (tokens, top_k), index), _vector(weights, "weights", torch.float32, (tokens, top_k), index)
+        n_out, room = tokens, 4 * n * o
         if work is None:
-            work = torch.empty(n * o, dtype=torch.float32, device=dev)
-        elif work.device != dev or not work.is_contiguous() or work.numel() * work.element_size() < room:
+            work = x.new_empty((n * o,), dtype=torch.float32)
+        elif work.get_device() != index or not work.is_contiguous() or work.numel() * work.element_size() < room:
             raise TardisError(1, "work must be a contiguous tensor of at least 4 rows o bytes on x's device")
-    px, ldx = _rows_of(x, "x", x.dtype, (nx, k), dev)
-    if W.dtype != x.dtype or W.device != dev or W.stride(2) != 1:
+        pwork = work.data_ptr()
+    if out is None:
+        out = x.new_empty((n_out, o), dtype=out_dtype)
+    px, ldx = _matrix(x, "x", dtype, nx, k, index)
+    stride_w, ldw, unit = W.stride()
+    if W.dtype is not dtype or W.get_device() != index or unit != 1:
         raise TardisError(1, "W must have x's dtype and device and unit inner stride")
-    py, ldy = _rows_of(out, "out", out_dtype, (n_out, o), dev)
-    pr, ldr = _rows_of(residual, "residual", out_dtype, (n_out, o), dev) if residual is not None else (None, 0)
-    i32 = torch.int32
-    desc = GroupedDesc(n, experts, k, o, _dtype_code(x.dtype), _dtype_code(out_dtype), act, px, ldx, nx, W.data_ptr(),
-                       W.stride(1) if o > 1 else k, W.stride(0), _vector(bias, "bias", torch.float32, (experts, o), dev),
-                       _vector(offsets, "offsets", i32, (experts + 1,), dev), _vector(rows, "rows", i32, (n,), dev), pr, ldr, py, ldy,
-                       tokens, top_k, _vector(slots, "slots", i32, (tokens, top_k), dev),
-                       _vector(weights, "weights", torch.float32, (tokens, top_k), dev), work.data_ptr() if room else None, room)
-    _check(load_library().tardis_grouped_linear(ctypes.byref(desc), _stream(stream)), what)
+    py, ldy = _matrix(out, "out", out_dtype, n_out, o, index)
+    pr, ldr = _matrix(residual, "residual", out_dtype, n_out, o, index) if residual is not None else (0, 0)
+    desc = _PACK_GROUPED(n, experts, k, o, code, out_code, act, px, ldx, nx, W.data_ptr(), ldw if o > 1 else k, stride_w,
+                         _vector(bias, "bias", torch.float32, (experts, o), index), _vector(offsets, "offsets", i32, (experts + 1,), index),
+                         _vector(rows, "rows", i32, (n,), index), pr, ldr, py, ldy, tokens, top_k, ps, pc, pwork, room)
+    status = load_library().tardis_grouped_linear(desc, _raw_stream(stream, index))
+    if status != TARDIS_OK:
+        _check(status, what)
     return out
 
 
@@ -299,23 +317,25 @@ def tardis_route(logits: torch.Tensor, top_k: int, normalise: bool = True, strea
     """The experts of every token (see tardis_route in tardis.h): logits float32 [tokens, experts] with unit inner stride.  Returns
     (experts int32 [tokens, top_k], weights float32 [tokens, top_k], offsets int32 [experts + 1], rows int32 [tokens top_k],
     slots int32 [tokens, top_k]): what tardis_grouped_linear and tardis_grouped_linear_combine take."""
-    dev = _operand_device(logits)
     if logits.dim() != 2:
         raise TardisError(1, "logits must be [tokens, experts]")
+    index = _current(logits)
     n, e = logits.shape
-    pl, ldl = _rows_of(logits, "logits", torch.float32, (n, e), dev)
+    pl, ldl = _matrix(logits, "logits", torch.float32, n, e, index)
     if not 1 <= top_k <= e:
         raise TardisError(1, "top_k must be between 1 and the number of experts")
     i32 = torch.int32
-    experts = torch.empty(n, top_k, dtype=i32, device=dev)
-    weights = torch.empty(n, top_k, dtype=torch.float32, device=dev)
-    offsets = torch.empty(e + 1, dtype=i32, device=dev)
-    rows = torch.empty(n * top_k, dtype=i32, device=dev)
-    slots = torch.empty(n, top_k, dtype=i32, device=dev)
-    work = torch.empty(256 * e, dtype=i32, device=dev) if n > 128 else None
-    _check(load_library().tardis_route(n, e, top_k, 1 if normalise else 0, pl, ldl, experts.data_ptr(), weights.data_ptr(),
-                                       offsets.data_ptr(), rows.data_ptr(), slots.data_ptr(), work.data_ptr() if work is not None else None,
-                                       1024 * e if work is not None else 0, _stream(stream)), "tardis_route")
+    experts = logits.new_empty((n, top_k), dtype=i32)
+    weights = logits.new_empty((n, top_k))
+    offsets = logits.new_empty((e + 1,), dtype=i32)
+    rows = logits.new_empty((n * top_k,), dtype=i32)
+    slots = logits.new_empty((n, top_k), dtype=i32)
+    work = logits.new_empty((256 * e,), dtype=i32) if n > 128 else None
+    status = load_library().tardis_route(n, e, top_k, 1 if normalise else 0, pl, ldl, experts.data_ptr(), weights.data_ptr(),
+                                         offsets.data_ptr(), rows.data_ptr(), slots.data_ptr(), work.data_ptr() if work is not None else 0,
+                                         1024 * e if work is not None else 0, _raw_stream(stream, index))
+    if status != TARDIS_OK:
+        _check(status, "tardis_route")
     return experts, weights, offsets, rows, slots
 
 

@@ -165,9 +165,9 @@ constexpr int FEW_ROWS = 8, FEW_WARPS = 8, FEW_U = 2;      // U: blocks of 64 ch
 
 __global__ void __launch_bounds__(FEW_WARPS * 32, 2) k_linear_few(const __grid_constant__ LinearArgs a) {
   constexpr int ROWS = FEW_ROWS, WARPS = FEW_WARPS, U = FEW_U;
-  extern __shared__ int table[];                           // starts, firsts (grouped only)
+  extern __shared__ int table[];                           // (grouped only)
   __shared__ float part[2][WARPS][ROWS][17];
-  int *const starts = table, *const firsts = table + a.groups + 1;
+  const Groups groups = groups_at(table, a.groups);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int nkb = (a.k + 63) / 64, ot = (a.o + 15) / 16;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -178,10 +178,10 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 2) k_linear_few(const __grid_c
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (a.offsets) {
-    build_groups(a.offsets, a.groups, a.n, ROWS, ot, starts, firsts);
+    build_groups(a.offsets, a.groups, a.n, ROWS, ot, groups);
     __syncthreads();
   }
-  const int items = a.offsets ? firsts[a.groups] : ot;
+  const int items = a.offsets ? groups.firsts[a.groups] : ot;
   const int from = int((long long)(blockIdx.x) * items / gridDim.x), to = int((long long)(blockIdx.x + 1) * items / gridDim.x);
   if (from == to) return;
 
@@ -189,11 +189,12 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 2) k_linear_few(const __grid_c
   auto locate = [&](int item) {
     Where w = {0, item * 16, 0, a.n};
     if (a.offsets) {
-      w.e = group_of(firsts, a.groups, item);
-      const int i = item - firsts[w.e], tile = i / ot;
+      const int place = place_of(groups, a.groups, item);
+      w.e = groups.order[place];
+      const int i = item - groups.firsts[place], tile = i / ot;
       w.o0 = (i - tile * ot) * 16;
-      w.first = starts[w.e] + tile * ROWS;
-      w.rows = min(ROWS, starts[w.e + 1] - w.first);
+      w.first = groups.starts[w.e] + tile * ROWS;
+      w.rows = min(ROWS, groups.starts[w.e + 1] - w.first);
     }
     return w;
   };
@@ -283,7 +284,7 @@ static tardis_status_t launch_few(const LinearArgs& a, cudaStream_t s) {
   const long long items = (long long)((a.o + 15) / 16) * (a.offsets ? a.n : 1);      // at most (a group's tile has a row)
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(items < 2 * sms ? items : 2 * sms)); cfg.blockDim = dim3(FEW_WARPS * 32); cfg.stream = s;
-  cfg.dynamicSmemBytes = a.offsets ? 8 * (a.groups + 1) : 0;
+  cfg.dynamicSmemBytes = a.offsets ? groups_bytes(a.groups) : 0;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -292,29 +293,67 @@ static tardis_status_t launch_few(const LinearArgs& a, cudaStream_t s) {
   return TARDIS_OK;
 }
 
-// A thread adds up one output of a token after the other, in the order of the token's choices.
-__global__ void __launch_bounds__(256) k_combine(const LinearArgs a, int top_k, const float* __restrict__ f, const int* __restrict__ slots,
-                                                 const float* __restrict__ weights) {
+// ---- the return to the tokens: bound by reading f ----
+// A thread adds up V outputs of a token, its choices in their order (four loads of f under way at a time).
+template <int V, typename O>
+__global__ void __launch_bounds__(256) k_combine(const __grid_constant__ LinearArgs a, int top_k, const float* __restrict__ f,
+                                                 const int* __restrict__ slots, const float* __restrict__ weights) {
   const long long t = blockIdx.x;
+  const int c = (blockIdx.y * 256 + threadIdx.x) * V;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (c >= a.o) return;
   const int lo = max(a.offsets[0], 0), hi = min(a.offsets[a.groups], a.n);
-  for (int c = blockIdx.y * 256 + threadIdx.x; c < a.o; c += gridDim.y * 256) {
-    float sum = 0.f;
-    for (int j = 0; j < top_k; ++j) {
-      const int slot = slots[t * top_k + j];
-      if (slot >= lo && slot < hi) sum = fmaf(weights[t * top_k + j], f[(long long)(slot) * a.o + c], sum);
+  Vec<V> sum = {};
+  struct alignas(sizeof(O) * V) Out { O v[V]; };
+  Out old;
+  if (a.res) old = *reinterpret_cast<const Out*>(static_cast<const O*>(a.res) + t * a.ldr + c);
+  for (int j0 = 0; j0 < top_k; j0 += 4) {
+    Vec<V> part[4];
+    float w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int slot = j0 + j < top_k ? slots[t * top_k + j0 + j] : -1;
+      const bool there = slot >= lo && slot < hi;
+      w[j] = there ? weights[t * top_k + j0 + j] : 0.f;
+      part[j] = there ? *reinterpret_cast<const Vec<V>*>(f + (long long)(slot) * a.o + c) : Vec<V>{};
     }
-    if (a.res) sum += load_out(a.res, t * a.ldr + c, a.out_dtype);
-    store_out(a.y, t * a.ldy + c, a.out_dtype, sum);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum.v[i] = fmaf(w[j], part[j].v[i], sum.v[i]);
   }
+  Out y;
+#pragma unroll
+  for (int i = 0; i < V; ++i) y.v[i] = from_f32<O>(a.res ? sum.v[i] + to_f32(old.v[i]) : sum.v[i]);
+  *reinterpret_cast<Out*>(static_cast<O*>(a.y) + t * a.ldy + c) = y;
+}
+
+template <int V, typename O>
+static tardis_status_t launch_combine_as(int tokens, int top_k, const LinearArgs& a, const float* f, const int* slots, const float* weights,
+                                         cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(tokens), unsigned((a.o + 256 * V - 1) / (256 * V))); cfg.blockDim = dim3(256); cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  TARDIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_combine<V, O>, a, top_k, f, slots, weights));
+  return TARDIS_OK;
 }
 
 }  // namespace linear
 
 tardis_status_t launch_combine(int tokens, int top_k, const LinearArgs& a, const float* f, const int* slots, const float* weights,
                                cudaStream_t s) {
-  linear::k_combine<<<dim3(unsigned(tokens), unsigned(a.o > 8192 ? 8 : (a.o + 1023) / 1024)), 256, 0, s>>>(a, top_k, f, slots, weights);
-  TARDIS_CUDA_TRY(cudaGetLastError());
-  return TARDIS_OK;
+  using namespace linear;
+  const size_t unit = a.out_dtype == TARDIS_BF16 ? 2 : 4;
+  auto fits = [&](const void* p, long long ld) { return !p || ((reinterpret_cast<uintptr_t>(p) | size_t(ld) * unit) & (4 * unit - 1)) == 0; };
+  const bool wide = a.o % 4 == 0 && fits(a.y, a.ldy) && fits(a.res, a.ldr);        // four outputs at a time
+  if (a.o > 65535 * 256) return TARDIS_ERR_UNSUPPORTED;
+  if (a.out_dtype == TARDIS_BF16)
+    return wide ? launch_combine_as<4, __nv_bfloat16>(tokens, top_k, a, f, slots, weights, s) : launch_combine_as<1, __nv_bfloat16>(tokens, top_k, a, f, slots, weights, s);
+  return wide ? launch_combine_as<4, float>(tokens, top_k, a, f, slots, weights, s) : launch_combine_as<1, float>(tokens, top_k, a, f, slots, weights, s);
 }
 
 tardis_status_t launch_linear(const LinearArgs& a, cudaStream_t s) {

@@ -80,45 +80,77 @@ __device__ __forceinline__ GroupTile find_group_tile(const int* offsets, int gro
   return t;
 }
 
-// The same as a table in shared memory, made by all threads of a CTA (callers synchronise afterwards): starts[e], where group e begins (its end is
-// starts[e + 1]), and firsts[e], the tiles in front of it when every `per` rows make `each` tiles.
-__device__ __forceinline__ void build_groups(const int* offsets, int groups, int n, int per, int each, int* starts, int* firsts) {
-  for (int e = threadIdx.x; e <= groups; e += blockDim.x) starts[e] = min(max(offsets[e], 0), n);
-  __syncthreads();
-  if (threadIdx.x >= 32) return;
-  const int lane = threadIdx.x;
-  int end = starts[0], before = 0;
-  __syncwarp();
-  for (int e0 = 0; e0 < groups; e0 += 32) {
-    const int e = e0 + lane;
-    int mine = e < groups ? max(starts[e + 1], end) : end;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int other = __shfl_up_sync(0xffffffffu, mine, d);
-      if (lane >= d) mine = max(mine, other);
-    }
-    int start = __shfl_up_sync(0xffffffffu, mine, 1);
-    if (lane == 0) start = end;
-    const int own = (mine - start + per - 1) / per * each;
-    int tiles = own;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int other = __shfl_up_sync(0xffffffffu, tiles, d);
-      if (lane >= d) tiles += other;
-    }
-    if (e < groups) { starts[e + 1] = mine; firsts[e] = before + tiles - own; }
-    end = __shfl_sync(0xffffffffu, mine, 31);
-    before += __shfl_sync(0xffffffffu, tiles, 31);
-    __syncwarp();
-  }
-  if (lane == 0) firsts[groups] = before;
+// The same as a table in shared memory, made by all threads of a CTA (callers synchronise afterwards).  The groups come in order of falling size where
+// there are at most kSorted of them (equal sizes in their own order): the tiles that take longest first, the tail of a launch is made of short ones.
+constexpr int kSorted = 256;
+struct Groups {
+  int* starts;      // [groups + 1] where group e begins; it ends at starts[e + 1]
+  int* firsts;      // [groups + 1] tiles in front of the i-th group of the order
+  int* order;       // [groups] the i-th group (before the table is complete: sizes)
+};
+__host__ __device__ constexpr int groups_bytes(int groups) { return 4 * (3 * groups + 2); }
+__device__ __forceinline__ Groups groups_at(void* p, int groups) {
+  int* const at = static_cast<int*>(p);
+  return {at, at + groups + 1, at + 2 * groups + 2};
 }
-// the group that has tile `tile` (below firsts[groups])
-__device__ __forceinline__ int group_of(const int* firsts, int groups, int tile) {
+// per: rows of a tile; each: tiles that so many rows make
+__device__ __forceinline__ void build_groups(const int* offsets, int groups, int n, int per, int each, Groups t) {
+  for (int e = threadIdx.x; e <= groups; e += blockDim.x) t.starts[e] = min(max(offsets[e], 0), n);
+  __syncthreads();
+  const int lane = threadIdx.x & 31;
+  if (threadIdx.x < 32) {
+    int end = t.starts[0];
+    __syncwarp();
+    for (int e0 = 0; e0 < groups; e0 += 32) {
+      const int e = e0 + lane;
+      int mine = e < groups ? max(t.starts[e + 1], end) : end;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int other = __shfl_up_sync(0xffffffffu, mine, d);
+        if (lane >= d) mine = max(mine, other);
+      }
+      if (e < groups) t.starts[e + 1] = mine;
+      end = __shfl_sync(0xffffffffu, mine, 31);
+      __syncwarp();
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < groups; e += blockDim.x) {
+    int place = e;
+    if (groups <= kSorted) {
+      const int size = t.starts[e + 1] - t.starts[e];
+      place = 0;
+      for (int f = 0; f < groups; ++f) {
+        const int other = t.starts[f + 1] - t.starts[f];
+        place += other > size || (other == size && f < e) ? 1 : 0;
+      }
+    }
+    t.order[place] = e;
+  }
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    int before = 0;
+    for (int i0 = 0; i0 < groups; i0 += 32) {
+      const int i = i0 + lane, e = i < groups ? t.order[i] : 0;
+      const int own = i < groups ? (t.starts[e + 1] - t.starts[e] + per - 1) / per * each : 0;
+      int tiles = own;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int other = __shfl_up_sync(0xffffffffu, tiles, d);
+        if (lane >= d) tiles += other;
+      }
+      if (i < groups) t.firsts[i] = before + tiles - own;
+      before += __shfl_sync(0xffffffffu, tiles, 31);
+    }
+    if (lane == 0) t.firsts[groups] = before;
+  }
+}
+// the place in the order of the group that has tile `tile` (below firsts[groups])
+__device__ __forceinline__ int place_of(const Groups& t, int groups, int tile) {
   int lo = 0, hi = groups;                                   // the last group whose first tile is not behind this one
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (firsts[mid] <= tile) lo = mid;
+    if (t.firsts[mid] <= tile) lo = mid;
     else hi = mid;
   }
   return lo;

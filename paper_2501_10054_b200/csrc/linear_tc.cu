@@ -31,7 +31,7 @@ template <int CTAS, int NT, int SPLITS> struct Cfg {
   static constexpr int A_BYTES = BM * BK * 2, B_ROWS = NT / CTAS, STAGE_BYTES = A_BYTES + B_ROWS * BK * 2;
   static constexpr int SHARE = (31 + SPLITS) / SPLITS;               // columns of a block of 32 that a CTA of the cluster finishes, at most
   static constexpr int EXCHANGE = SPLITS > 1 ? SPLITS * (NT / 32 * SHARE) * BM * 4 : 0;
-  static constexpr int NS = (204 * 1024 - EXCHANGE) / STAGE_BYTES;
+  static constexpr int NS = (200 * 1024 - EXCHANGE) / STAGE_BYTES;
   static constexpr int TMEM_COLS = 2 * NT;
   static constexpr int STEP = 16 * CTAS;                             // of N
   static constexpr int FIXED = NS * STAGE_BYTES + EXCHANGE + 1024 /* alignment slack */ + 256 /* barriers */;
@@ -83,18 +83,21 @@ template <int ACT> __device__ __forceinline__ float activation(float z) {
   return apply_act(z, ACT);
 }
 
-// Columns c .. c + 31 of a thread's channel: token c + i of the tile is row `row0 + c + i` of y.
+// Columns c .. c + 31 of a thread's channel (`count` of them): `row` is the row of y of the first.
 template <int ACT, typename O>
 __device__ __forceinline__ void finish(const LinearArgs& a, const float (&v)[32], long long row, int count, int o, float bias) {
   O* y = static_cast<O*>(a.y) + row * a.ldy + o;
   if (a.res) {
     const O* r = static_cast<const O*>(a.res) + row * a.ldr + o;
-    float old[32];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) old[i] = i < count ? to_f32(r[i * a.ldr]) : 0.f;
+    for (int i0 = 0; i0 < 32; i0 += 16) {                        // (sixteen loads at once)
+      float old[16];
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i < count) y[i * a.ldy] = from_f32<O>(activation<ACT>(v[i] + bias) + old[i]);
+      for (int i = 0; i < 16; ++i) old[i] = i0 + i < count ? to_f32(r[(i0 + i) * a.ldr]) : 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (i0 + i < count) y[(i0 + i) * a.ldy] = from_f32<O>(activation<ACT>(v[i0 + i] + bias) + old[i]);
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 32; ++i)
@@ -128,8 +131,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   uint64_t* parts_empty = parts_full + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(parts_empty + 1);
   volatile uint32_t* failed = tmem_slot + 1;
-  int* const starts = reinterpret_cast<int*>(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE + 256);   // [groups + 1] first rows (grouped only)
-  int* const firsts = starts + p.a.groups + 1;                                                     // [groups + 1] first tiles
+  const Groups groups = groups_at(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE + 256, p.a.groups);     // (grouped only)
   static_assert((2 * C::NS + 6) * 8 + 8 <= 256, "");
 
   const LinearArgs& a = p.a;
@@ -152,24 +154,25 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");             // (x, offsets, ... may come from the launch before)
   int ntiles;
-  if (a.offsets) build_groups(a.offsets, a.groups, a.n, NT, mt, starts, firsts);
+  if (a.offsets) build_groups(a.offsets, a.groups, a.n, NT, mt, groups);
   tc_fence_before();
   __syncthreads();
   if (in_cluster > 1) cluster_sync();                            // (the other CTAs' barriers are reported to)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (this CTA has its tensor memory)
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  ntiles = a.offsets ? firsts[a.groups] : (a.n + NT - 1) / NT * mt;
+  ntiles = a.offsets ? groups.firsts[a.groups] : (a.n + NT - 1) / NT * mt;
 
   auto decode = [&](int tile) {
     Tile t;
     t.e = 0;
     int group_first = 0, group_rows = a.n, rem = tile;
     if (a.offsets) {
-      t.e = group_of(firsts, a.groups, tile);
-      rem = tile - firsts[t.e];
-      group_first = starts[t.e];
-      group_rows = starts[t.e + 1] - group_first;
+      const int place = place_of(groups, a.groups, tile);
+      t.e = groups.order[place];
+      rem = tile - groups.firsts[place];
+      group_first = groups.starts[t.e];
+      group_rows = groups.starts[t.e + 1] - group_first;
     }
     const int tiles = (group_rows + NT - 1) / NT;
     const int per = ((group_rows + tiles - 1) / tiles + C::STEP - 1) & ~(C::STEP - 1);         // tokens per tile: as even as the steps allow
@@ -400,10 +403,10 @@ static tardis_status_t launch(const LinearArgs& a, int dev, int sms, cudaStream_
   const long long mt = (a.o + BM * CTAS - 1) / (BM * CTAS), nt = (a.n + NT - 1) / NT;
   p.tokens_fast = nt <= mt ? 1 : 0;
   p.band = 8;
-  const int smem = C::FIXED + (a.offsets ? 8 * (a.groups + 1) : 0);
+  const int smem = C::FIXED + (a.offsets ? groups_bytes(a.groups) : 0);
   static thread_local int room_on = -1;               // the device on which this thread last gave the kernel its shared memory
   if (dev != room_on) {
-    TARDIS_CUDA_TRY(cudaFuncSetAttribute(k_linear_tc<CTAS, NT, SPLITS, GATHER>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::FIXED + 8 * (kMaxExperts + 1)));
+    TARDIS_CUDA_TRY(cudaFuncSetAttribute(k_linear_tc<CTAS, NT, SPLITS, GATHER>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::FIXED + groups_bytes(kMaxExperts)));
     room_on = dev;
   }
   long long tiles = (nt + (a.offsets ? (a.groups < a.n ? a.groups : a.n) : 0)) * mt;     // at most

@@ -477,6 +477,14 @@ def test_route_refuses(lib):
     assert route(e=1025, ldl=1025) == 2 and route(e=64, k=33, ldl=64) == 2 and route(n=1 << 30) == 2
 
 
+def test_packed_descriptors_have_the_layout_of_the_structures():
+    import ctypes
+    assert len(T._PACK_LINEAR(*range(15))) == ctypes.sizeof(T.LinearDesc) and len(T._PACK_GROUPED(*range(26))) == ctypes.sizeof(T.GroupedDesc)
+    for pack, desc in ((T._PACK_LINEAR, T.LinearDesc), (T._PACK_GROUPED, T.GroupedDesc)):
+        d = desc.from_buffer_copy(pack(*range(1, len(desc._fields_) + 1)))
+        assert [getattr(d, name) for name, _ in desc._fields_] == list(range(1, len(desc._fields_) + 1))
+
+
 @gpu
 def test_binding_refuses():
     x, W, b, r = make(4, 64, 24, BF)
