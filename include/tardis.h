@@ -252,7 +252,7 @@ tardis_status_t tardis_grouped_linear(const tardis_grouped_desc_t* desc, tardis_
  *   offsets    out, device [n_experts + 1]: where each expert's rows begin; the last is the number of pairs
  *   rows       out, device [n_tokens top_k]: the token of every sorted pair; -1 behind the last
  *   slots      out, device [n_tokens, top_k]: the place of every pair among them
- *   work       device scratch of 1024 n_experts bytes, caller-owned; may be NULL for up to 128 tokens
+ *   work       device scratch of 4096 n_experts bytes, caller-owned; may be NULL for up to 128 tokens
  * 1 <= top_k <= 32, top_k <= n_experts <= 1024, n_tokens top_k < 2^31 (UNSUPPORTED beyond).  Asynchronous on `stream`;
  * allocates nothing; nothing is kept; the same bits from run to run.  Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
 tardis_status_t tardis_route(int64_t n_tokens, int32_t n_experts, int32_t top_k, int32_t normalise, const float* logits, int64_t ldl,

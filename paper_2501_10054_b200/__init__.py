@@ -325,15 +325,13 @@ def tardis_route(logits: torch.Tensor, top_k: int, normalise: bool = True, strea
     if not 1 <= top_k <= e:
         raise TardisError(1, "top_k must be between 1 and the number of experts")
     i32 = torch.int32
-    experts = logits.new_empty((n, top_k), dtype=i32)
-    weights = logits.new_empty((n, top_k))
+    experts, slots, rows, weights = logits.new_empty((4, n, top_k), dtype=i32).unbind(0)       # (one allocation)
+    rows, weights = rows.view(-1), weights.view(torch.float32)
     offsets = logits.new_empty((e + 1,), dtype=i32)
-    rows = logits.new_empty((n * top_k,), dtype=i32)
-    slots = logits.new_empty((n, top_k), dtype=i32)
-    work = logits.new_empty((256 * e,), dtype=i32) if n > 128 else None
+    work = logits.new_empty((1024 * e,), dtype=i32) if n > 128 else None
     status = load_library().tardis_route(n, e, top_k, 1 if normalise else 0, pl, ldl, experts.data_ptr(), weights.data_ptr(),
                                          offsets.data_ptr(), rows.data_ptr(), slots.data_ptr(), work.data_ptr() if work is not None else 0,
-                                         1024 * e if work is not None else 0, _raw_stream(stream, index))
+                                         4096 * e if work is not None else 0, _raw_stream(stream, index))
     if status != TARDIS_OK:
         _check(status, "tardis_route")
     return experts, weights, offsets, rows, slots

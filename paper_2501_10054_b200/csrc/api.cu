@@ -428,7 +428,7 @@ tardis_status_t tardis_route(int64_t n_tokens, int32_t n_experts, int32_t top_k,
   const void* all[] = {logits, experts, weights, offsets, rows, slots, work};
   for (const void* p : all)
     if (reinterpret_cast<uintptr_t>(p) & 3u) return TARDIS_ERR_INVALID_ARG;
-  if (n_tokens > 128 && (!work || work_bytes < size_t(1024) * size_t(n_experts))) return TARDIS_ERR_INVALID_ARG;
+  if (n_tokens > 128 && (!work || work_bytes < size_t(4096) * size_t(n_experts))) return TARDIS_ERR_INVALID_ARG;
   return launch_route(int(n_tokens), n_experts, top_k, normalise, logits, ldl, experts, weights, offsets, rows, slots,
                       static_cast<int*>(work), reinterpret_cast<cudaStream_t>(stream));
 }

@@ -473,7 +473,7 @@ def test_route_refuses(lib):
     assert route(logits=None) == 1 and route(logits=(1 << 19) + 1) == 1
     for i in range(5):
         assert route(outs=p[:i] + [None] + p[i + 1:]) == 1 and route(outs=p[:i] + [p[i] + 2] + p[i + 1:]) == 1
-    assert route(n=129) == 1 and route(n=129, work=1 << 25, bytes=1024 * 8 - 1) == 1
+    assert route(n=129) == 1 and route(n=129, work=1 << 25, bytes=4096 * 8 - 1) == 1
     assert route(e=1025, ldl=1025) == 2 and route(e=64, k=33, ldl=64) == 2 and route(n=1 << 30) == 2
 
 
