@@ -1,12 +1,12 @@
 // The router of expert-grouped products: per token the top_k largest logits and their softmax weights, and all (token, choice) pairs sorted
 // by expert, stable in the token.
 //
-// A warp takes a token: its logits lie in registers (lane l holds experts l, l + 32, ...; the next token's are loaded meanwhile), each of top_k rounds takes
-// the largest value by a warp-wide maximum over an order-preserving integer image and then the lowest expert that has it.  Sorting is counting: a
-// part of the tokens counts its choices per expert, the places of a part's pairs start behind those of all smaller experts and of the same expert in
-// earlier parts, and inside a block of 128 tokens the earlier tokens of an expert are the set bits below the token's in the expert's bit mask.  Up to
-// 128 tokens are one launch; more are two: choices and counts of small parts (two tokens per warp of 16: the rounds are a chain of latencies), then the
-// places.  Nothing waits for another CTA and no order of atomics shows in the result.
+// 8, 16 or 32 lanes take a token: its logits lie in registers (lane l of L holds experts l, l + L, ...; the next token's are loaded meanwhile), each of top_k
+// rounds takes the largest value by a maximum over an order-preserving integer image and then the lowest expert that has it.  (A warp per token
+// executes three times the instructions for 64 experts and four choices: 10 us for 16384 tokens.)  Sorting is counting: a part of the tokens counts its
+// choices per expert, the places of a part's pairs start behind those of all smaller experts and of the same expert in earlier parts, and inside a block
+// of 128 tokens the earlier tokens of an expert are the set bits below the token's in the expert's bit mask.  Up to 128 tokens are one launch; more
+// are two: choices and counts of small parts, then the places.  Nothing waits for another CTA and no order of atomics shows in the result.
 #include <limits.h>
 #include <math_constants.h>
 
@@ -34,57 +34,62 @@ __device__ __forceinline__ uint32_t ordered(float f) {
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
 constexpr uint32_t kNone = 0x007fffffu;                   // ordered(-inf)
 
-template <int PER> __device__ __forceinline__ void fetch(const Params& p, long long t, int lane, float (&f)[PER]) {
+template <int L> __device__ __forceinline__ uint32_t most_of(uint32_t v) {          // over the L lanes of a token
+  if constexpr (L == 32) return __reduce_max_sync(0xffffffffu, v);
+  else {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) f[i] = lane + 32 * i < p.experts ? p.logits[t * p.ldl + lane + 32 * i] : -CUDART_INF_F;
+    for (int d = L / 2; d > 0; d >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+  }
 }
-// Top-k of one token by a converged warp; lane j < top_k returns its j-th choice (-1: none left) and writes it with its weight.
-template <int PER> __device__ __forceinline__ int choose(const Params& p, long long t, int lane, const float (&f)[PER]) {
+template <int L> __device__ __forceinline__ float sum_of(float v) {
+#pragma unroll
+  for (int d = L / 2; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
+template <int L, int PER> __device__ __forceinline__ void fetch(const Params& p, long long t, bool there, int l, float (&f)[PER]) {
+#pragma unroll
+  for (int i = 0; i < PER; ++i) f[i] = there && l + L * i < p.experts ? p.logits[t * p.ldl + l + L * i] : -CUDART_INF_F;
+}
+// Top-k of the tokens of a converged warp (32 / L of them); lane l < top_k of a token returns its l-th choice (-1: none left) and writes it with its
+// weight where the token is there.
+template <int L, int PER> __device__ __forceinline__ int choose(const Params& p, long long t, bool there, int l, const float (&f)[PER]) {
   uint32_t v[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) v[i] = f[i] == f[i] ? ordered(f[i] + 0.f) : kNone;       // NaN is no candidate; -0 is +0
-  // softmax over all: the sum before candidates leave
-  uint32_t most = v[0];
-#pragma unroll
-  for (int i = 1; i < PER; ++i) most = max(most, v[i]);
-  most = __reduce_max_sync(0xffffffffu, most);
-  const float top = unordered(most);
-  float total = 0.f;
-  if (!p.normalise && most > kNone) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (v[i] > kNone) total += v[i] == most ? 1.f : expf(unordered(v[i]) - top);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-  }
+  uint32_t most = kNone;
+  float top = 0.f, total = 0.f, share = 0.f;
   int mine = -1;
-  float share = 0.f;
   for (int j = 0; j < p.top_k; ++j) {
     uint32_t best = v[0];
 #pragma unroll
     for (int i = 1; i < PER; ++i) best = max(best, v[i]);
-    best = __reduce_max_sync(0xffffffffu, best);
-    if (best <= kNone) break;                             // (uniform)
-    int at = INT_MAX;
+    best = most_of<L>(best);
+    uint32_t at = 0xffffffffu;                            // the lowest expert that has it, as its complement
 #pragma unroll
     for (int i = PER - 1; i >= 0; --i)
-      if (v[i] == best) at = lane + 32 * i;
-    at = int(__reduce_min_sync(0xffffffffu, unsigned(at)));
+      if (v[i] == best) at = l + L * i;
+    at = ~most_of<L>(~at);
+    if (j == 0) {
+      most = best;
+      top = unordered(most);
+      if (!p.normalise) {                                 // softmax over all: the sum before candidates leave
+#pragma unroll
+        for (int i = 0; i < PER; ++i) total += v[i] == kNone ? 0.f : v[i] == most ? 1.f : expf(unordered(v[i]) - top);
+        total = sum_of<L>(total);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-      if (at == lane + 32 * i) v[i] = kNone;
-    if (lane == j) { mine = at; share = best == most ? 1.f : expf(unordered(best) - top); }
+      if (at == uint32_t(l + L * i)) v[i] = kNone;
+    if (l == j && best != kNone) { mine = int(at); share = best == most ? 1.f : expf(unordered(best) - top); }
   }
-  if (p.normalise) {
-    total = share;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+  if (p.normalise) total = sum_of<L>(share);
+  if (there && l < p.top_k) {
+    p.chosen[t * p.top_k + l] = mine;
+    p.weights[t * p.top_k + l] = mine >= 0 ? share / total : 0.f;
   }
-  if (lane < p.top_k) {
-    p.chosen[t * p.top_k + lane] = mine;
-    p.weights[t * p.top_k + lane] = mine >= 0 ? share / total : 0.f;
-  }
-  return mine;
+  return there && l < p.top_k ? mine : -1;
 }
 
 // Exclusive prefix sum of cnt[0 .. experts) into out[0 .. experts], by one warp.
@@ -139,11 +144,11 @@ __device__ __forceinline__ void fill_rest(const Params& p, int from, int step0, 
 }
 
 // ONLY: the whole call in this launch (32 warps); otherwise choices and counts
-template <int PER, bool ONLY> __global__ void __launch_bounds__(ONLY ? 1024 : 512) k_choose(const __grid_constant__ Params p) {
+template <int L, int PER, bool ONLY> __global__ void __launch_bounds__(ONLY ? 1024 : 512) k_choose(const __grid_constant__ Params p) {
   extern __shared__ int sm[];
   int* const count = sm;                                  // [experts]
   int* const chosen = sm + 6 * p.experts + 1;             // ONLY: [kBlock][top_k]
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % L, each = blockDim.x / L;      // each: tokens at a time
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   for (int e = threadIdx.x; e < p.experts; e += blockDim.x) count[e] = 0;
   __syncthreads();
@@ -151,12 +156,13 @@ template <int PER, bool ONLY> __global__ void __launch_bounds__(ONLY ? 1024 : 51
   const long long t0 = (long long)(blockIdx.x) * p.part;
   const int n = int(min((long long)(p.part), p.tokens - t0));
   float f[PER], g[PER];
-  if (warp < n) fetch<PER>(p, t0 + warp, lane, f);
-  for (int i = warp; i < n; i += warps) {
-    if (i + warps < n) fetch<PER>(p, t0 + i + warps, lane, g);
-    const int e = choose<PER>(p, t0 + i, lane, f);
+  int i = threadIdx.x / L;
+  fetch<L, PER>(p, t0 + i, i < n, l, f);
+  for (int w = warp * (32 / L); w < n; w += each, i += each) {                  // (w: the warp's first token)
+    if (w + each < n) fetch<L, PER>(p, t0 + i + each, i + each < n, l, g);
+    const int e = choose<L, PER>(p, t0 + i, i < n, l, f);
     if (e >= 0) atomicAdd(&count[e], 1);
-    if (ONLY && lane < p.top_k) chosen[i * p.top_k + lane] = e;
+    if (ONLY && i < n && l < p.top_k) chosen[i * p.top_k + l] = e;
 #pragma unroll
     for (int j = 0; j < PER; ++j) f[j] = g[j];
   }
@@ -232,9 +238,9 @@ static tardis_status_t launch(void (*kernel)(Params), const Params& p, int block
   TARDIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
   return TARDIS_OK;
 }
-template <int PER> static tardis_status_t launch_choose(const Params& p, cudaStream_t s) {
-  if (p.parts == 1) return launch(k_choose<PER, true>, p, 1, 1024, 6 * p.experts + 1 + kBlock * p.top_k, s);
-  return launch(k_choose<PER, false>, p, p.parts, 512, p.experts, s);
+template <int L, int PER> static tardis_status_t launch_choose(const Params& p, cudaStream_t s) {
+  if (p.parts == 1) return launch(k_choose<L, PER, true>, p, 1, 1024, 6 * p.experts + 1 + kBlock * p.top_k, s);
+  return launch(k_choose<L, PER, false>, p, p.parts, 512, p.experts, s);
 }
 
 }  // namespace route
@@ -243,14 +249,16 @@ tardis_status_t launch_route(int tokens, int experts, int top_k, int normalise, 
                              float* weights, int* offsets, int* rows, int* slots, int* work, cudaStream_t s) {
   using namespace route;
   Params p = {tokens, experts, top_k, normalise, kBlock, 1, 1, logits, ldl, chosen, weights, offsets, rows, slots, work};
+  const bool narrow = top_k <= 8 && experts <= 64, half = top_k <= 16 && experts <= 128;
   if (tokens > kBlock) {
-    p.part = 32;
+    p.part = narrow ? 64 : 32;                             // one or two passes of a CTA's 16 warps
     while ((tokens - 1) / p.part >= kMaxParts) p.part *= 2;
     p.parts = (tokens - 1) / p.part + 1;
     p.per_place = p.part < kBlock ? kBlock / p.part : 1;
   }
-  tardis_status_t st = experts <= 32 ? launch_choose<1>(p, s) : experts <= 64 ? launch_choose<2>(p, s) : experts <= 128 ? launch_choose<4>(p, s)
-                     : experts <= 256 ? launch_choose<8>(p, s) : launch_choose<32>(p, s);
+  tardis_status_t st = narrow ? (experts <= 8 ? launch_choose<8, 1>(p, s) : experts <= 32 ? launch_choose<8, 4>(p, s) : launch_choose<8, 8>(p, s))
+                     : half ? launch_choose<16, 8>(p, s) : experts <= 128 ? launch_choose<32, 4>(p, s)
+                     : experts <= 256 ? launch_choose<32, 8>(p, s) : launch_choose<32, 32>(p, s);
   if (st == TARDIS_OK && p.parts > 1)
     st = launch(k_place, p, (p.parts - 1) / p.per_place + 1, 512, 7 * experts + 1 + kBlock * top_k, s);
   return st;
