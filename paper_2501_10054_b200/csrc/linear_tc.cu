@@ -26,20 +26,26 @@ using namespace tc;
 
 constexpr int BM = 128, BK = 64, BOX = 32;       // channels of a CTA's tile; k per stage; rows per copy of tokens
 constexpr int NTHREADS = 320, GATHER_WARPS = 4;
+constexpr int TURN = 5;                          // k blocks by which the channel tiles of a few tokens are apart, see decode()
+
+constexpr int STAGING_LD = 36, STAGING_WARP = 16 * STAGING_LD * 4;    // 16 columns x 32 channels of a warp
 
 template <int CTAS, int NT, int SPLITS> struct Cfg {
   static constexpr int A_BYTES = BM * BK * 2, B_ROWS = NT / CTAS, STAGE_BYTES = A_BYTES + B_ROWS * BK * 2;
   static constexpr int SHARE = (31 + SPLITS) / SPLITS;               // columns of a block of 32 that a CTA of the cluster finishes, at most
   static constexpr int EXCHANGE = SPLITS > 1 ? SPLITS * (NT / 32 * SHARE) * BM * 4 : 0;
-  static constexpr int NS = (200 * 1024 - EXCHANGE) / STAGE_BYTES;
+  static constexpr int STAGING = SPLITS > 1 ? 0 : 8 * STAGING_WARP;                    // the epilogue's, see finish
+  static constexpr int NS = (212 * 1024 - EXCHANGE - STAGING) / STAGE_BYTES;
   static constexpr int TMEM_COLS = 2 * NT;
   static constexpr int STEP = 16 * CTAS;                             // of N
-  static constexpr int FIXED = NS * STAGE_BYTES + EXCHANGE + 1024 /* alignment slack */ + 256 /* barriers */;
+  static_assert(NS >= 4, "");
+  static constexpr int FIXED = NS * STAGE_BYTES + EXCHANGE + STAGING + 1024 /* alignment slack */ + 256 /* barriers */;
 };
 
 struct Params {
   LinearArgs a;
   int kblocks, band, tokens_fast;
+  int wide;                        // y (and the residual) can be stored 16 bytes at a time
 };
 
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
@@ -76,41 +82,84 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* b, uint32_t parity) 
 }
 
 // One tile as a role sees it.
-struct Tile { int e, o0, first, rows, nt; };     // group, first output, first row, rows, columns of the MMA
+struct Tile { int e, o0, first, rows, nt, turn; };     // group, first output, first row, rows, columns of the MMA, k block to begin with
 
 template <int ACT> __device__ __forceinline__ float activation(float z) {
   if (ACT == TARDIS_ACT_GELU_TANH) return gelu_tanh_f32(z);
   return apply_act(z, ACT);
 }
 
-// Columns c .. c + 31 of a thread's channel (`count` of them): `row` is the row of y of the first.
+// The epilogue takes sixteen columns of a warp's 32 channels o0 .. o0 + 31 at a time through shared memory (`stage`, column-major), `count` of them rows of y
+// from `row` on.  Where y and the residual are aligned and all channels are inside, a lane has 8 channels of a token and touches both 16 bytes at a
+// time, the residual of the next sixteen columns on its way; else its own channel of one token after the other.  (Two bytes per lane throughout: the
+// epilogue of 1024 x 64 x 16384 with a residual took 51 us, with the residual read when it is needed 35.)
+template <typename O> struct Eight { uint4 piece[sizeof(O) / 2]; };
+template <typename O> struct alignas(16) Out8 { O v[8]; };
+template <typename O>
+__device__ __forceinline__ void read_residual(const LinearArgs& a, long long row, int count, int o0, int lane, Eight<O> (&old)[2]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < int(sizeof(O) / 2); ++i)
+      if (h * 8 + (lane >> 2) < count)
+        old[h].piece[i] = reinterpret_cast<const uint4*>(static_cast<const O*>(a.res) + (row + h * 8 + (lane >> 2)) * a.ldr + o0 + (lane & 3) * 8)[i];
+}
 template <int ACT, typename O>
-__device__ __forceinline__ void finish(const LinearArgs& a, const float (&v)[32], long long row, int count, int o, float bias) {
-  O* y = static_cast<O*>(a.y) + row * a.ldy + o;
-  if (a.res) {
-    const O* r = static_cast<const O*>(a.res) + row * a.ldr + o;
+__device__ __forceinline__ void finish(const LinearArgs& a, bool wide, long long row, int count, int o0, const float* stage, int lane, const Eight<O> (&old)[2]) {
+  if (wide) {
+    const int c = lane >> 2, ch = (lane & 3) * 8;                // this lane's column of 8 and its channels
 #pragma unroll
-    for (int i0 = 0; i0 < 32; i0 += 16) {                        // (sixteen loads at once)
-      float old[16];
+    for (int h = 0; h < 2; ++h) {
+      const int col = h * 8 + c;
+      if (col >= count) continue;
+      const float4 lo = *reinterpret_cast<const float4*>(stage + col * STAGING_LD + ch);
+      const float4 hi = *reinterpret_cast<const float4*>(stage + col * STAGING_LD + ch + 4);
+      const float z[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+      Out8<O> y;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) old[i] = i0 + i < count ? to_f32(r[(i0 + i) * a.ldr]) : 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i0 + i < count) y[(i0 + i) * a.ldy] = from_f32<O>(activation<ACT>(v[i0 + i] + bias) + old[i]);
+      for (int i = 0; i < 8; ++i) {
+        float v = activation<ACT>(z[i]);
+        if (a.res) v += to_f32(reinterpret_cast<const Out8<O>*>(&old[h])->v[i]);
+        y.v[i] = from_f32<O>(v);
+      }
+      *reinterpret_cast<Out8<O>*>(static_cast<O*>(a.y) + (row + col) * a.ldy + o0 + ch) = y;
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i < count) y[i * a.ldy] = from_f32<O>(activation<ACT>(v[i] + bias));
+  } else if (o0 + lane < a.o) {
+    O* const y = static_cast<O*>(a.y) + o0 + lane;
+    const O* const r = static_cast<const O*>(a.res) + o0 + lane;
+#pragma unroll 4
+    for (int i = 0; i < min(count, 16); ++i) {
+      float v = activation<ACT>(stage[i * STAGING_LD + lane]);
+      if (a.res) v += to_f32(r[(row + i) * a.ldr]);
+      y[(row + i) * a.ldy] = from_f32<O>(v);
+    }
   }
 }
-template <typename O>
-__device__ __forceinline__ void finish_act(const LinearArgs& a, const float (&v)[32], long long row, int count, int o, float bias) {
-  switch (a.act) {
-    case TARDIS_ACT_GELU_TANH: finish<TARDIS_ACT_GELU_TANH, O>(a, v, row, count, o, bias); break;
-    case TARDIS_ACT_GELU_ERF: finish<TARDIS_ACT_GELU_ERF, O>(a, v, row, count, o, bias); break;
-    case TARDIS_ACT_RELU: finish<TARDIS_ACT_RELU, O>(a, v, row, count, o, bias); break;
-    default: finish<TARDIS_ACT_NONE, O>(a, v, row, count, o, bias);
+// A warp's share of a tile: columns first, first + step, ... in blocks of 16 of the accumulator at `tacc`.  wait() returns whether it has been computed.
+template <typename O, typename Wait>
+__device__ __forceinline__ void finish_tile(const LinearArgs& a, bool wide, long long row, int rows, int first, int step, int o0, float bias, uint32_t tacc, float* stage,
+                                            int lane, Wait wait) {
+  Eight<O> old[2], next[2];
+  const bool ahead = wide && a.res;
+  if (ahead) read_residual<O>(a, row + first, rows - first, o0, lane, next);
+  const bool ok = wait();
+#pragma unroll 1
+  for (int c = first; c < rows; c += step) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) old[h] = next[h];
+    if (ahead) read_residual<O>(a, row + c + step, rows - c - step, o0, lane, next);
+    float v[16];
+    tmem_ld16(tacc + uint32_t(c), v);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) stage[i * STAGING_LD + lane] = ok ? v[i] + bias : CUDART_NAN_F;
+    __syncwarp();
+    switch (a.act) {
+      case TARDIS_ACT_GELU_TANH: finish<TARDIS_ACT_GELU_TANH, O>(a, wide, row + c, rows - c, o0, stage, lane, old); break;
+      case TARDIS_ACT_GELU_ERF: finish<TARDIS_ACT_GELU_ERF, O>(a, wide, row + c, rows - c, o0, stage, lane, old); break;
+      case TARDIS_ACT_RELU: finish<TARDIS_ACT_RELU, O>(a, wide, row + c, rows - c, o0, stage, lane, old); break;
+      default: finish<TARDIS_ACT_NONE, O>(a, wide, row + c, rows - c, o0, stage, lane, old);
+    }
+    __syncwarp();
   }
 }
 
@@ -123,7 +172,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* const exchange = reinterpret_cast<float*>(smem + C::NS * C::STAGE_BYTES);      // [SPLITS][NT / 32 * SHARE][128]
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE + C::STAGING);
   uint64_t* empty = full + C::NS;
   uint64_t* accum_full = empty + C::NS;        // [2]
   uint64_t* accum_empty = accum_full + 2;      // [2]
@@ -131,7 +180,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   uint64_t* parts_empty = parts_full + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(parts_empty + 1);
   volatile uint32_t* failed = tmem_slot + 1;
-  const Groups groups = groups_at(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE + 256, p.a.groups);     // (grouped only)
+  const Groups groups = groups_at(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE + C::STAGING + 256, p.a.groups);     // (grouped only)
   static_assert((2 * C::NS + 6) * 8 + 8 <= 256, "");
 
   const LinearArgs& a = p.a;
@@ -163,6 +212,10 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   const uint32_t tmem_base = *tmem_slot;
   ntiles = a.offsets ? groups.firsts[a.groups] : (a.n + NT - 1) / NT * mt;
 
+  // this CTA's part of the k blocks
+  const int per_split = SPLIT ? (p.kblocks + SPLITS - 1) / SPLITS : p.kblocks;
+  const int kb_lo = SPLIT ? min(rank * per_split, p.kblocks) : 0, nkb = SPLIT ? min(p.kblocks, kb_lo + per_split) - kb_lo : p.kblocks;
+
   auto decode = [&](int tile) {
     Tile t;
     t.e = 0;
@@ -185,13 +238,12 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     t.o0 = mi * (BM * CTAS) + (CTAS == 2 ? rank * BM : 0);
     t.first = group_first + ni * per;
     t.rows = max(0, min(per, group_rows - ni * per));
+    // A few tokens are read by all channel tiles at once: each begins at a block of its own, so that they do not all ask for the same lines (us in step / apart:
+    // 64 tokens of 4096 -> 16384 27.2 / 26.3, 128 30.4 / 28.6, 256 36.6 / 35.4; where clusters share the channels 64 of 16384 -> 4096 30.3 / 32.1).
+    t.turn = !SPLIT && tiles == 1 ? mi * TURN % nkb : 0;
     t.nt = max(C::STEP, (t.rows + C::STEP - 1) & ~(C::STEP - 1));
     return t;
   };
-  // this CTA's part of the k blocks
-  const int per_split = SPLIT ? (p.kblocks + SPLITS - 1) / SPLITS : p.kblocks;
-  const int kb_lo = SPLIT ? min(rank * per_split, p.kblocks) : 0, nkb = SPLIT ? min(p.kblocks, kb_lo + per_split) - kb_lo : p.kblocks;
-
   int issued = 0;
   if (warp == 0) {
     // ---------------- copies ----------------
@@ -206,7 +258,9 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         ++issued;
         uint8_t* const sa = smem + s * C::STAGE_BYTES;
         uint8_t* const sb = sa + C::A_BYTES;
-        const int kx = kb * BK;
+        int kx = kb + t.turn;                                    // (the turned order ends with the blocks in front of its beginning)
+        if (kx >= kb_lo + nkb) kx -= nkb;
+        kx *= BK;
         if (elect_one()) {
           if (rank == 0 || CTAS == 1) mbar_expect_tx(&full[s], CTAS * bytes);
           if (CTAS == 2) tma_load_3d_pair(sa, &tmW, kx, t.o0, t.e, in_rank_0(&full[s]));
@@ -273,21 +327,24 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         }
       for (int kb = kb_lo; kb < kb_lo + nkb; ++kb) {
         if (!mbar_wait_issue(&empty[s], parity, failed)) break;
+        int kx = kb + t.turn;
+        if (kx >= kb_lo + nkb) kx -= nkb;
         if (elect_one()) {
           uint8_t* const sb = smem + s * C::STAGE_BYTES + C::A_BYTES + w * 512;
 #pragma unroll
           for (int j = 0; j < QUADS; ++j)
             if ((w + j * GATHER_WARPS) * 4 < half) {
-              if (CTAS == 2) tma_gather4_pair(sb + j * (GATHER_WARPS * 512), &tmX, kb * BK, idx[j], in_rank_0(&full[s]));
-              else tma_gather4(sb + j * (GATHER_WARPS * 512), &tmX, kb * BK, idx[j], &full[s]);
+              if (CTAS == 2) tma_gather4_pair(sb + j * (GATHER_WARPS * 512), &tmX, kx * BK, idx[j], in_rank_0(&full[s]));
+              else tma_gather4(sb + j * (GATHER_WARPS * 512), &tmX, kx * BK, idx[j], &full[s]);
             }
         }
         if (++s == C::NS) { s = 0; parity ^= 1; }
       }
     }
   } else {
-    // ---------------- epilogue: a warp has TMEM lanes 32 (warp % 4) .. + 31 and every other block of 32 columns ----------------
+    // ---------------- epilogue: a warp has TMEM lanes 32 (warp % 4) .. + 31 and every other block of columns ----------------
     const int q = warp & 3, half = (warp - 2) >> 2;
+    float* const staging = reinterpret_cast<float*>(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE + (warp - 2) * STAGING_WARP);
     uint32_t use = 0;
     bool ok = true;
     for (int tile = first_tile; tile < ntiles; tile += step) {
@@ -295,22 +352,18 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       const int o = t.o0 + q * 32 + lane;
       const uint32_t ab = use & 1u;
       const float bias = a.bias && o < a.o ? a.bias[(long long)(t.e) * a.o + o] : 0.f;
-      if (nkb > 0) ok = ok && mbar_wait_warp(&accum_full[ab], (use >> 1) & 1);
-      if (!ok) *failed = 1u;
-      tc_fence_after();
+      auto computed = [&]() {
+        if (nkb > 0) ok = ok && mbar_wait_warp(&accum_full[ab], (use >> 1) & 1);
+        if (!ok) *failed = 1u;
+        tc_fence_after();
+        return ok;
+      };
       if (!SPLIT) {
-        for (int c = half * 32; c < t.rows; c += 64) {
-          float v[32];
-          tmem_ld32(tmem_base + ab * NT + (uint32_t(q * 32) << 16) + uint32_t(c), v);
-          if (!ok) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = CUDART_NAN_F;
-          }
-          if (o < a.o) {
-            if (a.out_dtype == TARDIS_BF16) finish_act<__nv_bfloat16>(a, v, t.first + c, t.rows - c, o, bias);
-            else finish_act<float>(a, v, t.first + c, t.rows - c, o, bias);
-          }
-        }
+        const int o0 = o - lane;
+        const bool wide = p.wide && o0 + 32 <= a.o;
+        const uint32_t tacc = tmem_base + ab * NT + (uint32_t(q * 32) << 16);
+        if (a.out_dtype == TARDIS_BF16) finish_tile<__nv_bfloat16>(a, wide, t.first, t.rows, half * 16, 32, o0, bias, tacc, staging, lane, computed);
+        else finish_tile<float>(a, wide, t.first, t.rows, half * 16, 32, o0, bias, tacc, staging, lane, computed);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
@@ -318,6 +371,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
           else mbar_arrive(&accum_empty[ab]);
         }
       } else {
+        computed();
         // of every block of 32 columns, column i belongs to CTA i % SPLITS; the parts of the tile before have been taken by then
         if (use > 0 && ok) ok = mbar_wait_cluster(parts_empty, (use - 1) & 1);
         constexpr int SHARE = C::SHARE, WIDTH = NT / 32 * SHARE;
@@ -396,6 +450,7 @@ static bool make_weight_map(CUtensorMap* map, const LinearArgs& a) {
 template <int CTAS, int NT, int SPLITS, bool GATHER>
 static tardis_status_t launch(const LinearArgs& a, int dev, int sms, cudaStream_t s) {
   using C = Cfg<CTAS, NT, SPLITS>;
+  static_assert(C::FIXED + groups_bytes(kMaxExperts) <= 227 * 1024, "");
   CUtensorMap w, x;
   if (!make_weight_map(&w, a) || !make_map(&x, a.x, a.nx, a.k, a.ldx, GATHER ? 1 : BOX)) return TARDIS_ERR_INVALID_ARG;
   Params p;
@@ -403,6 +458,9 @@ static tardis_status_t launch(const LinearArgs& a, int dev, int sms, cudaStream_
   const long long mt = (a.o + BM * CTAS - 1) / (BM * CTAS), nt = (a.n + NT - 1) / NT;
   p.tokens_fast = nt <= mt ? 1 : 0;
   p.band = 8;
+  const size_t unit = a.out_dtype == TARDIS_BF16 ? 2 : 4;
+  auto fits = [&](const void* q, long long ld) { return !q || ((reinterpret_cast<uintptr_t>(q) | size_t(ld) * unit) & 15) == 0; };
+  p.wide = fits(a.y, a.ldy) && fits(a.res, a.ldr);
   const int smem = C::FIXED + (a.offsets ? groups_bytes(a.groups) : 0);
   static thread_local int room_on = -1;               // the device on which this thread last gave the kernel its shared memory
   if (dev != room_on) {
