@@ -220,8 +220,9 @@ tardis_status_t tardis_linear(const tardis_linear_desc_t* desc, tardis_stream_t 
  *              offset before: groups never overlap or leave the outputs, whatever the array holds);
  *   rows       device [n_rows] or NULL; an index outside 0 .. n_x - 1 reads as a row of zeros;
  *   W          [n_experts][o, k]: experts stride_w elements apart (a multiple of 8, at least (o - 1) ldw + k);
- *   work       with slots: device scratch of at least 4 n_rows o bytes, 16-byte aligned, caller-owned (calls that overlap
- *              in time need one each); else ignored.
+ *   work       device scratch, 16-byte aligned, caller-owned (calls that overlap in time need one each).  With slots at
+ *              least 4 n_rows o bytes.  Else it may be NULL; with rows of bf16 and 2 n_rows k bytes or more, long calls
+ *              gather the rows there once instead of picking them again for every tile of outputs.
  * Other arguments, alignment, result and errors as for tardis_linear; n_experts <= 1024 (UNSUPPORTED beyond). */
 typedef struct {
   int64_t n_rows;             /* rows of f: (token, choice) pairs; below 2^31 */
@@ -234,7 +235,7 @@ typedef struct {
   const int32_t* rows;
   const void* residual; int64_t ldr;            /* as y */
   void* y; int64_t ldy;       /* [n_rows, o], with slots [n_tokens, o] */
-  int64_t n_tokens;           /* the rest: with slots only */
+  int64_t n_tokens;           /* with slots only, to weights */
   int32_t top_k;
   const int32_t* slots;       /* [n_tokens, top_k] */
   const float* weights;       /* [n_tokens, top_k] */

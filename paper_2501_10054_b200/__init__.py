@@ -277,6 +277,9 @@ def _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, back, wor
         elif work.get_device() != index or not work.is_contiguous() or work.numel() * work.element_size() < room:
             raise TardisError(1, "work must be a contiguous tensor of at least 4 rows o bytes on x's device")
         pwork = work.data_ptr()
+    elif rows is not None and n >= 1024 and dtype is torch.bfloat16:
+        work, room = x.new_empty((n, k)), 2 * n * k
+        pwork = work.data_ptr()
     if out is None:
         out = x.new_empty((n_out, o), dtype=out_dtype)
     px, ldx = _matrix(x, "x", dtype, nx, k, index)

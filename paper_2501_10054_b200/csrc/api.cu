@@ -405,7 +405,11 @@ tardis_status_t tardis_grouped_linear(const tardis_grouped_desc_t* d, tardis_str
   if (!a.offsets || d->n_x < (a.rows ? 1 : d->n_rows) || (reinterpret_cast<uintptr_t>(a.offsets) | reinterpret_cast<uintptr_t>(a.rows)) & 3u) return TARDIS_ERR_INVALID_ARG;
   if (!linear_pointers_ok(a, d->n_x, out_rows)) return TARDIS_ERR_INVALID_ARG;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (!back) return launch_linear(a, s);
+  if (!back) {
+    if (d->work && !aligned16(d->work)) return TARDIS_ERR_INVALID_ARG;
+    if (d->work_bytes >= size_t(a.n) * size_t(a.k) * 2) a.work = d->work;
+    return launch_linear(a, s);
+  }
   if ((reinterpret_cast<uintptr_t>(d->slots) | reinterpret_cast<uintptr_t>(d->weights)) & 3u) return TARDIS_ERR_INVALID_ARG;
   const size_t room = size_t(a.n) * size_t(a.o) * 4;
   if (room > 0 && (!d->work || !aligned16(d->work) || d->work_bytes < room)) return TARDIS_ERR_INVALID_ARG;

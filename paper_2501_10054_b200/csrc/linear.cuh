@@ -19,6 +19,7 @@ struct LinearArgs {
   void* y; long long ldy;
   int groups;                        // 1 without offsets
   const int* offsets;                // [groups + 1] or null (one group of all rows)
+  void* work;                        // with rows: [n, k] in bf16, where they may be gathered, or null
   const int* rows;                   // [n] or null: row r of the product takes row rows[r] of x (zeros where that is outside [0, nx))
 };
 

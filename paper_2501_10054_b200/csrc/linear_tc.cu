@@ -15,6 +15,7 @@
 //
 // Every wait on an mbarrier is bounded: when it runs out the CTA stops issuing, fills what it would have written with NaN and ends after its copies have landed.
 #include <cuda.h>
+#include <math.h>
 #include <math_constants.h>
 
 #include "linear.cuh"
@@ -26,14 +27,14 @@ using namespace tc;
 
 constexpr int BM = 128, BK = 64, BOX = 32;       // channels of a CTA's tile; k per stage; rows per copy of tokens
 constexpr int NTHREADS = 320, GATHER_WARPS = 4;
-constexpr int TURN = 5;                          // k blocks by which the channel tiles of a few tokens are apart, see decode()
 
 constexpr int STAGING_LD = 36, STAGING_WARP = 16 * STAGING_LD * 4;    // 16 columns x 32 channels of a warp
 
 template <int CTAS, int NT, int SPLITS> struct Cfg {
   static constexpr int A_BYTES = BM * BK * 2, B_ROWS = NT / CTAS, STAGE_BYTES = A_BYTES + B_ROWS * BK * 2;
-  static constexpr int SHARE = (31 + SPLITS) / SPLITS;               // columns of a block of 32 that a CTA of the cluster finishes, at most
-  static constexpr int EXCHANGE = SPLITS > 1 ? SPLITS * (NT / 32 * SHARE) * BM * 4 : 0;
+  static constexpr int SHARE = (7 + SPLITS) / SPLITS;                // of the 8 quads of columns in a block of 32, how many a CTA of the cluster finishes at most
+  static constexpr int PART_LD = NT / 32 * SHARE * 4 + 4;            // floats of a channel in a part (4 apart from a multiple of 8: no bank conflicts)
+  static constexpr int EXCHANGE = SPLITS > 1 ? SPLITS * BM * PART_LD * 4 : 0;
   static constexpr int STAGING = SPLITS > 1 ? 0 : 8 * STAGING_WARP;                    // the epilogue's, see finish
   static constexpr int NS = (212 * 1024 - EXCHANGE - STAGING) / STAGE_BYTES;
   static constexpr int TMEM_COLS = 2 * NT;
@@ -84,8 +85,20 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* b, uint32_t parity) 
 // One tile as a role sees it.
 struct Tile { int e, o0, first, rows, nt, turn; };     // group, first output, first row, rows, columns of the MMA, k block to begin with
 
-template <int ACT> __device__ __forceinline__ float activation(float z) {
+// The erf form for outputs of 16 bits: z Phi(z) = max(z, 0) - |z| / 2 erfc(|z| / sqrt 2), erfc by formula 7.1.26 of Abramowitz and Stegun (absolute error below
+// 1.5e-7; no difference of numbers near 1 in the negative tail).  777 tokens of 4544 -> 18176 with erff took 128 us.
+__device__ __forceinline__ float gelu_erf_short(float z) {
+  const float x = fabsf(z) * 0.7071067811865476f, t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
+  float poly = fmaf(1.061405429f, t, -1.453152027f);
+  poly = fmaf(poly, t, 1.421413741f);
+  poly = fmaf(poly, t, -0.284496736f);
+  poly = fmaf(poly, t, 0.254829592f);
+  const float half = 0.5f * z;
+  return (half + fabsf(half)) - fminf(fabsf(half), 3.0e38f) * (poly * t * __expf(-x * x));
+}
+template <int ACT, typename O> __device__ __forceinline__ float activation(float z) {
   if (ACT == TARDIS_ACT_GELU_TANH) return gelu_tanh_f32(z);
+  if (ACT == TARDIS_ACT_GELU_ERF && sizeof(O) == 2) return gelu_erf_short(z);
   return apply_act(z, ACT);
 }
 
@@ -118,7 +131,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, bool wide, long long
       Out8<O> y;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        float v = activation<ACT>(z[i]);
+        float v = activation<ACT, O>(z[i]);
         if (a.res) v += to_f32(reinterpret_cast<const Out8<O>*>(&old[h])->v[i]);
         y.v[i] = from_f32<O>(v);
       }
@@ -129,7 +142,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, bool wide, long long
     const O* const r = static_cast<const O*>(a.res) + o0 + lane;
 #pragma unroll 4
     for (int i = 0; i < min(count, 16); ++i) {
-      float v = activation<ACT>(stage[i * STAGING_LD + lane]);
+      float v = activation<ACT, O>(stage[i * STAGING_LD + lane]);
       if (a.res) v += to_f32(r[(row + i) * a.ldr]);
       y[(row + i) * a.ldy] = from_f32<O>(v);
     }
@@ -171,7 +184,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   static_assert(!(SPLIT && CTAS == 2) && C::B_ROWS <= 128, "");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* const exchange = reinterpret_cast<float*>(smem + C::NS * C::STAGE_BYTES);      // [SPLITS][NT / 32 * SHARE][128]
+  float* const exchange = reinterpret_cast<float*>(smem + C::NS * C::STAGE_BYTES);      // [SPLITS][128][PART_LD]
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE + C::STAGING);
   uint64_t* empty = full + C::NS;
   uint64_t* accum_full = empty + C::NS;        // [2]
@@ -238,9 +251,9 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     t.o0 = mi * (BM * CTAS) + (CTAS == 2 ? rank * BM : 0);
     t.first = group_first + ni * per;
     t.rows = max(0, min(per, group_rows - ni * per));
-    // A few tokens are read by all channel tiles at once: each begins at a block of its own, so that they do not all ask for the same lines (us in step / apart:
-    // 64 tokens of 4096 -> 16384 27.2 / 26.3, 128 30.4 / 28.6, 256 36.6 / 35.4; where clusters share the channels 64 of 16384 -> 4096 30.3 / 32.1).
-    t.turn = !SPLIT && tiles == 1 ? mi * TURN % nkb : 0;
+    // A few tokens are read by all channel tiles at once: every other one begins in the middle of its channels, so that they do not all ask for the same lines (us in
+    // step / apart: 64 tokens of 4096 -> 16384 27.0 / 25.0, 128 29.9 / 27.7, 64 of 16384 -> 4096 29.3 / 28.3).
+    t.turn = tiles == 1 && (mi & 1) ? nkb >> 1 : 0;
     t.nt = max(C::STEP, (t.rows + C::STEP - 1) & ~(C::STEP - 1));
     return t;
   };
@@ -371,21 +384,35 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
           else mbar_arrive(&accum_empty[ab]);
         }
       } else {
+        constexpr int SHARE = C::SHARE, QUADS = NT / 32 * SHARE, LD = C::PART_LD;
+        // this CTA finishes two quads of columns at a time, their residuals loaded ahead
+        float old[8], next[8];
+        auto read_old = [&](int w0) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int w = w0 + j / 4, i = w % SHARE * SPLITS + rank, c = w / SHARE * 32 + i * 4 + j % 4;
+            next[j] = a.res && o < a.o && w < QUADS && i < 8 && c < t.rows ? load_out(a.res, (t.first + c) * a.ldr + o, a.out_dtype) : 0.f;
+          }
+        };
+        read_old(half * 2);
         computed();
-        // of every block of 32 columns, column i belongs to CTA i % SPLITS; the parts of the tile before have been taken by then
+        // of every block of 32 columns, quad i (four columns) belongs to CTA i % SPLITS; the parts of the tile before have been taken by then
         if (use > 0 && ok) ok = mbar_wait_cluster(parts_empty, (use - 1) & 1);
-        constexpr int SHARE = C::SHARE, WIDTH = NT / 32 * SHARE;
         uint32_t to[SPLITS];
 #pragma unroll
-        for (int r = 0; r < SPLITS; ++r) to[r] = in_rank(exchange + rank * WIDTH * BM + q * 32 + lane, r);
+        for (int r = 0; r < SPLITS; ++r) to[r] = in_rank(exchange + (rank * BM + q * 32 + lane) * LD, r);
         for (int c = half * 32; c < t.rows; c += 64) {
           float v[32];
           tmem_ld32(tmem_base + ab * NT + (uint32_t(q * 32) << 16) + uint32_t(c), v);
+          if (!ok || nkb == 0) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (c + i < t.rows)
-              asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to[i % SPLITS] + uint32_t(c / 32 * SHARE + i / SPLITS) * (BM * 4)),
-                           "f"(!ok ? CUDART_NAN_F : nkb > 0 ? v[i] : 0.f) : "memory");
+            for (int i = 0; i < 32; ++i) v[i] = ok ? 0.f : CUDART_NAN_F;
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (c + 4 * i < t.rows)
+              asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to[i % SPLITS] + uint32_t(c / 32 * SHARE + i / SPLITS) * 16),
+                           "f"(v[4 * i]), "f"(v[4 * i + 1]), "f"(v[4 * i + 2]), "f"(v[4 * i + 3]) : "memory");
         }
         tc_fence_before();
         __syncwarp();
@@ -396,27 +423,28 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         }
         ok = mbar_wait_cluster(parts_full, use & 1) && ok;
         if (!ok) *failed = 1u;
-        // this CTA's columns, eight at a time (the loads of eight residuals at once)
-        for (int w0 = half * 8; w0 < WIDTH; w0 += 16) {
-          float old[8];
-          bool mine[8];
+        for (int w0 = half * 2; w0 < QUADS; w0 += 4) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int w = w0 + j, i = w % SHARE * SPLITS + rank, c = w / SHARE * 32 + i;
-            mine[j] = w < WIDTH && i < 32 && c < t.rows && o < a.o;
-            old[j] = mine[j] && a.res ? load_out(a.res, (t.first + c) * a.ldr + o, a.out_dtype) : 0.f;
-          }
+          for (int j = 0; j < 8; ++j) old[j] = next[j];
+          read_old(w0 + 4);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            if (!mine[j]) continue;
-            const int w = w0 + j, c = w / SHARE * 32 + w % SHARE * SPLITS + rank;
-            float z = 0.f;
+          for (int h = 0; h < 2; ++h) {
+            const int w = w0 + h, i = w % SHARE * SPLITS + rank, c = w / SHARE * 32 + i * 4;
+            if (w >= QUADS || i >= 8 || c >= t.rows || o >= a.o) continue;
+            float z[4] = {};
 #pragma unroll
-            for (int r = 0; r < SPLITS; ++r) z += exchange[(r * WIDTH + w) * BM + q * 32 + lane];
-            z += bias;
-            z = a.act == TARDIS_ACT_GELU_TANH ? gelu_tanh_f32(z) : apply_act(z, a.act);
-            if (a.res) z += old[j];
-            store_out(a.y, (t.first + c) * a.ldy + o, a.out_dtype, ok ? z : CUDART_NAN_F);
+            for (int r = 0; r < SPLITS; ++r) {
+              const float4 part = *reinterpret_cast<const float4*>(exchange + (r * BM + q * 32 + lane) * LD + w * 4);
+              z[0] += part.x; z[1] += part.y; z[2] += part.z; z[3] += part.w;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if (c + j >= t.rows) break;
+              float y = z[j] + bias;
+              y = a.act == TARDIS_ACT_GELU_TANH ? gelu_tanh_f32(y) : apply_act(y, a.act);
+              if (a.res) y += old[h * 4 + j];
+              store_out(a.y, (t.first + c + j) * a.ldy + o, a.out_dtype, ok ? y : CUDART_NAN_F);
+            }
           }
         }
         __syncwarp();
@@ -497,24 +525,78 @@ static tardis_status_t launch_splits(const LinearArgs& a, int splits, int dev, i
   return launch_rows<1, NT, 1>(a, dev, sms, s);
 }
 
+// a.work[r] = x[a.rows[r]], a warp per row: 16 bytes per lane
+__global__ void __launch_bounds__(256) k_gather_rows(const __grid_constant__ LinearArgs a) {
+  const int r = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, pieces = a.k / 8;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (r >= a.n || r < a.offsets[0] || r >= a.offsets[a.groups]) return;
+  const int src = a.rows[r];
+  const bool there = src >= 0 && src < a.nx;
+  const uint4* const from = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.x) + (there ? src : 0) * a.ldx);
+  uint4* const to = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.work) + (long long)(r) * a.k);
+  for (int i0 = lane; i0 < pieces; i0 += 128) {
+    uint4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = there && i0 + 32 * j < pieces ? from[i0 + 32 * j] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i0 + 32 * j < pieces) to[i0 + 32 * j] = v[j];
+  }
+}
+static tardis_status_t launch_gather_rows(const LinearArgs& a, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned((a.n - 1) / 8 + 1)); cfg.blockDim = dim3(256); cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  TARDIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_gather_rows, a));
+  return TARDIS_OK;
+}
+
 }  // namespace linear
 
-tardis_status_t launch_linear_tc(const LinearArgs& a, cudaStream_t s) {
+tardis_status_t launch_linear_tc(const LinearArgs& given, cudaStream_t s) {
   using namespace linear;
+  LinearArgs a = given;
   if (!tensor_maps_available()) return TARDIS_ERR_UNSUPPORTED;
   int dev = 0, sms = 0;
   TARDIS_CUDA_TRY(cudaGetDevice(&dev));
   TARDIS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-  const long long groups = a.groups, per_group = (a.n + groups - 1) / groups;
-  const long long pair_tiles = ((a.o + 255) / 256) * (a.offsets ? groups * ((per_group + 255) / 256) : (a.n + 255) / 256);
-  if (per_group > 128 && pair_tiles * 2 * 10 >= sms * 7) return launch_rows<2, 256, 1>(a, dev, sms, s);
-  const long long tiles = ((a.o + 127) / 128) * (a.offsets ? groups : 1);
+  // The variant with the shortest estimate.  A CTA takes some 0.235 us per block of 64 k (less than its MMAs only with 256 tokens), all of them
+  // together the time of the weights that they read at once at 6.3 TB/s; clusters of 2, 3 and 4 leave SMs of a GPC unused.  What a launch takes beside
+  // that, and a further wave of clusters that exchange parts, is measured too.  (Estimate / measured, us: 128 tokens of 4096 -> 4096, splits of 2 of 64 tokens 15.5 / 15.5, of 4
+  // of 128 16.3 / 17.1, whole 64 19.5 / 18.6, 128 20.6 / 20.6; 160 of 4096 -> 16384, 128 35.6 / 37.4, pairs 29.5 / 30.5; 512 of 4096 -> 1024, 4 of 128 14.8 / 15.8.)
   const int kblocks = (a.k + BK - 1) / BK;
-  const bool narrow = per_group <= 64;
-  const long long all = narrow ? tiles : tiles * ((per_group + 127) / 128);
-  int splits = 4;
-  while (splits > 1 && (all * splits > (splits == 4 ? 132 : sms) || kblocks / splits < 4)) --splits;
-  return narrow ? launch_splits<64>(a, splits, dev, sms, s) : launch_splits<128>(a, splits, dev, sms, s);
+  const long long groups = a.offsets ? (a.groups < a.n ? a.groups : a.n) : 1, rows = (a.n + groups - 1) / groups;
+  const double clusters[5] = {0., double(sms), sms / 2., sms * 0.304, sms * 0.223};       // of 1 .. 4 CTAs at once
+  struct Choice { int kind, splits; double us; } best = {2, 1, 1e30};                     // kind: 0, 1: 64 or 128 tokens; 2: pairs, 256
+  for (int kind = 0; kind < 3; ++kind)
+    for (int splits = 1; splits <= (kind == 2 ? 1 : 4); ++splits) {
+      if (splits > 1 && kblocks < 4 * splits) continue;
+      const int ctas = kind == 2 ? 2 : 1, most = 64 << kind;
+      const long long cuts = (rows + most - 1) / most, tiles = (a.o + BM * ctas - 1) / (BM * ctas) * cuts * groups;
+      const double width = double((rows + cuts - 1) / cuts), at_once = floor(clusters[splits * ctas]);
+      const double waves = ceil(tiles / at_once), running = tiles < at_once ? double(tiles) : at_once;
+      double step = fmax(0.235, running / cuts * (splits * ctas) * (BM * BK * 2) / 6.3e6);
+      if (kind == 2) step = fmax(step, fmax(0.245, 0.275 * width / 256));
+      if (a.rows) step = fmax(step, 0.0035 * width / ctas);                                // (rows picked one by one)
+      double us = waves * ((kblocks + splits - 1) / splits) * step;
+      us += splits == 1 ? 4.0 + 0.012 * width : (kind == 0 ? 8. : 11.) + 4. * (waves - 1);
+      if (us < best.us) best = {kind, splits, us};
+    }
+  if (best.kind == 2) {
+    // Every tile of 256 outputs picks its rows again, at a third of the rate of whole boxes: with scratch they are picked once (8192 rows of 4096 -> 16384: 957 us picked
+    // tile by tile, 784 without picking).
+    if (a.rows && a.work && a.o > 1024) {
+      const tardis_status_t st = launch_gather_rows(a, s);
+      if (st != TARDIS_OK) return st;
+      a.x = a.work; a.ldx = a.k; a.nx = a.n; a.rows = nullptr;
+    }
+    return launch_rows<2, 256, 1>(a, dev, sms, s);
+  }
+  return best.kind == 1 ? launch_splits<128>(a, best.splits, dev, sms, s) : launch_splits<64>(a, best.splits, dev, sms, s);
 }
 
 }  // namespace tardis
