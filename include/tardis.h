@@ -194,11 +194,11 @@ tardis_status_t tardis_gemm_bf16(int32_t M, int32_t N, int32_t K, const void* A,
  * y may be residual (in place, with ldr = ldy) and overlaps none of the other inputs.  n = 0 does nothing.  Asynchronous
  * on `stream`; allocates nothing; nothing is kept; the same bits from run to run.  (Should a wait inside the tensor-core
  * kernel run out, which no valid call makes happen, the tile concerned is filled with NaN.)
- * Errors: INVALID_ARG, UNSUPPORTED (driver without tensor-map support; more than some 4 million rows of fp32), CUDA. */
+ * Errors: INVALID_ARG, UNSUPPORTED (driver without tensor-map support; more than 8 million outputs of fp32), CUDA. */
 #define TARDIS_ACT_NONE (-1)
 typedef struct {
-  int64_t n;                  /* rows of x and y (tokens); below 2^31 */
-  int32_t k, o;               /* channels in and out */
+  int64_t n;                  /* rows of x and y (tokens); below 2^31 - 4096 */
+  int32_t k, o;               /* channels in and out, up to 2^30 */
   int32_t dtype, out_dtype, act;
   const void* x; int64_t ldx; /* [n, k] */
   const void* W; int64_t ldw; /* [o, k], the nn.Linear layout */
@@ -225,7 +225,7 @@ tardis_status_t tardis_linear(const tardis_linear_desc_t* desc, tardis_stream_t 
  *              gather the rows there once instead of picking them again for every tile of outputs.
  * Other arguments, alignment, result and errors as for tardis_linear; n_experts <= 1024 (UNSUPPORTED beyond). */
 typedef struct {
-  int64_t n_rows;             /* rows of f: (token, choice) pairs; below 2^31 */
+  int64_t n_rows;             /* rows of f: (token, choice) pairs; below 2^31 - 4096 */
   int32_t n_experts, k, o;
   int32_t dtype, out_dtype, act;
   const void* x; int64_t ldx; int64_t n_x;      /* [n_x, k] */

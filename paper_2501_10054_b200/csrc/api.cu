@@ -346,8 +346,8 @@ tardis_status_t tardis_gemm_bf16(int32_t M, int32_t N, int32_t K, const void* A,
 
 // What tardis_linear and tardis_grouped_linear ask of their arguments alike.
 static bool linear_args_ok(const LinearArgs& a, long long n, long long nx, long long out_rows) {
-  constexpr long long kMost = 1ll << 31;
-  if (n < 0 || n >= kMost || nx < 0 || nx >= kMost || out_rows < 0 || out_rows >= kMost || a.k <= 0 || a.o <= 0) return false;
+  constexpr long long kMost = (1ll << 31) - 4096;            // (rows rounded up to tiles still are 32-bit numbers)
+  if (n < 0 || n >= kMost || nx < 0 || nx >= kMost || out_rows < 0 || out_rows >= kMost || a.k <= 0 || a.o <= 0 || a.k > 1 << 30 || a.o > 1 << 30) return false;
   if (a.dtype != TARDIS_F32 && a.dtype != TARDIS_BF16) return false;
   if (a.out_dtype != TARDIS_F32 && a.out_dtype != a.dtype) return false;
   if (a.act != TARDIS_ACT_NONE && a.act != TARDIS_ACT_GELU_TANH && a.act != TARDIS_ACT_GELU_ERF && a.act != TARDIS_ACT_RELU) return false;

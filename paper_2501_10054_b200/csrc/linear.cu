@@ -14,9 +14,9 @@ template <int T>
 __global__ void __launch_bounds__(256) k_linear_f32(const __grid_constant__ LinearArgs a) {
   constexpr int TILE = 16 * T, BK = 16, LD = TILE + 4, PER = TILE * BK / 4 / 256 + (TILE * BK / 4 % 256 != 0);     // PER: 16-byte loads per thread and operand
   __shared__ __align__(16) float sw[BK][LD], sx[BK][LD];
-  const GroupTile t = find_group_tile(a.offsets, a.groups, a.n, TILE, blockIdx.y);
+  const GroupTile t = find_group_tile(a.offsets, a.groups, a.n, TILE, blockIdx.x);
   if (t.rows == 0) return;
-  const int o0 = blockIdx.x * TILE, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;      // tx: outputs, ty: rows
+  const int o0 = blockIdx.y * TILE, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;      // tx: outputs, ty: rows
   const float *w[PER], *x[PER];                              // this thread's rows of W and x (null: zeros), four channels at a time
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
@@ -82,8 +82,9 @@ template <int T>
 static tardis_status_t launch_f32_tiles(const LinearArgs& a, cudaStream_t s) {
   const int tile = 16 * T;
   const long long tiles = (a.n + tile - 1) / tile + (a.offsets ? (a.groups < a.n ? a.groups : a.n) : 0);     // at most
-  if (tiles > 65535) return TARDIS_ERR_UNSUPPORTED;
-  k_linear_f32<T><<<dim3(unsigned((a.o + tile - 1) / tile), unsigned(tiles)), 256, 0, s>>>(a);
+  const int outputs = (a.o + tile - 1) / tile;
+  if (outputs > 65535) return TARDIS_ERR_UNSUPPORTED;
+  k_linear_f32<T><<<dim3(unsigned(tiles), unsigned(outputs)), 256, 0, s>>>(a);
   TARDIS_CUDA_TRY(cudaGetLastError());
   return TARDIS_OK;
 }
@@ -151,7 +152,7 @@ static tardis_status_t launch_f32(const LinearArgs& a, cudaStream_t s) {
   const long long groups = a.offsets ? a.groups : 1, rows = (a.n + groups - 1) / groups;
   auto tiles = [&](int tile) { return (a.o + tile - 1) / tile * (groups * ((rows + tile - 1) / tile)); };
   if (tiles(128) >= 148) return launch_f32_tiles<8>(a, s);
-  return tiles(64) >= 148 || a.n > 1000000 ? launch_f32_tiles<4>(a, s) : launch_f32_tiles<2>(a, s);
+  return tiles(64) >= 148 ? launch_f32_tiles<4>(a, s) : launch_f32_tiles<2>(a, s);
 }
 
 // ---- up to eight rows of bf16: bound by reading the weights once ----

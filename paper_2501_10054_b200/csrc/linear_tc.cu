@@ -471,6 +471,9 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
 }
 
 // ---- host side ------------------------------------------------------------------------------------------
+// Clusters of one CTA per SM that run at once: of three and four the SMs of a GPC leave a rest (45 and 33 of 148 SMs, as the occupancy query says).
+static long long clusters_at_once(int sms, int ctas) { return ctas <= 2 ? sms / ctas : (long long)(sms * (ctas == 3 ? 0.305 : 0.223)); }
+
 static bool make_weight_map(CUtensorMap* map, const LinearArgs& a) {
   return make_map_3d(map, a.W, a.o, a.groups, a.k, a.ldw, a.groups > 1 ? a.stride_w : a.ldw, BM);
 }
@@ -497,7 +500,7 @@ static tardis_status_t launch(const LinearArgs& a, int dev, int sms, cudaStream_
   }
   long long tiles = (nt + (a.offsets ? (a.groups < a.n ? a.groups : a.n) : 0)) * mt;     // at most
   constexpr int in_cluster = SPLITS * CTAS;
-  const long long at_once = sms / in_cluster;
+  const long long at_once = clusters_at_once(sms, in_cluster);
   if (tiles > at_once) tiles = at_once;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(tiles * in_cluster)); cfg.blockDim = dim3(NTHREADS + (GATHER ? 32 * GATHER_WARPS : 0)); cfg.dynamicSmemBytes = smem; cfg.stream = s;
@@ -566,30 +569,29 @@ tardis_status_t launch_linear_tc(const LinearArgs& given, cudaStream_t s) {
   TARDIS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   // The variant with the shortest estimate.  A CTA takes some 0.235 us per block of 64 k (less than its MMAs only with 256 tokens), all of them
   // together the time of the weights that they read at once at 6.3 TB/s; clusters of 2, 3 and 4 leave SMs of a GPC unused.  What a launch takes beside
-  // that, and a further wave of clusters that exchange parts, is measured too.  (Estimate / measured, us: 128 tokens of 4096 -> 4096, splits of 2 of 64 tokens 15.5 / 15.5, of 4
-  // of 128 16.3 / 17.1, whole 64 19.5 / 18.6, 128 20.6 / 20.6; 160 of 4096 -> 16384, 128 35.6 / 37.4, pairs 29.5 / 30.5; 512 of 4096 -> 1024, 4 of 128 14.8 / 15.8.)
+  // that, and a further wave of clusters that exchange parts, is measured too.  (Estimate / measured, us: 128 tokens of 4096 -> 4096, splits of 2 of 64 tokens 16.8 / 15.5, of 4
+  // of 128 18.5 / 17.1, whole 64 19.8 / 18.6, 128 20.6 / 20.6; 160 of 4096 -> 16384, 128 35.0 / 37.4, pairs 27.0 / 30.5; 512 of 4096 -> 1024, 4 of 128 16.9 / 15.8.)
   const int kblocks = (a.k + BK - 1) / BK;
   const long long groups = a.offsets ? (a.groups < a.n ? a.groups : a.n) : 1, rows = (a.n + groups - 1) / groups;
-  const double clusters[5] = {0., double(sms), sms / 2., sms * 0.304, sms * 0.223};       // of 1 .. 4 CTAs at once
   struct Choice { int kind, splits; double us; } best = {2, 1, 1e30};                     // kind: 0, 1: 64 or 128 tokens; 2: pairs, 256
   for (int kind = 0; kind < 3; ++kind)
     for (int splits = 1; splits <= (kind == 2 ? 1 : 4); ++splits) {
       if (splits > 1 && kblocks < 4 * splits) continue;
       const int ctas = kind == 2 ? 2 : 1, most = 64 << kind;
       const long long cuts = (rows + most - 1) / most, tiles = (a.o + BM * ctas - 1) / (BM * ctas) * cuts * groups;
-      const double width = double((rows + cuts - 1) / cuts), at_once = floor(clusters[splits * ctas]);
+      const double width = double((rows + cuts - 1) / cuts), at_once = double(clusters_at_once(sms, splits * ctas));
       const double waves = ceil(tiles / at_once), running = tiles < at_once ? double(tiles) : at_once;
       double step = fmax(0.235, running / cuts * (splits * ctas) * (BM * BK * 2) / 6.3e6);
       if (kind == 2) step = fmax(step, fmax(0.245, 0.275 * width / 256));
       if (a.rows) step = fmax(step, 0.0035 * width / ctas);                                // (rows picked one by one)
       double us = waves * ((kblocks + splits - 1) / splits) * step;
-      us += splits == 1 ? 4.0 + 0.012 * width : (kind == 0 ? 8. : 11.) + 4. * (waves - 1);
+      us += splits == 1 ? 4.0 + 0.012 * width : waves * (3.5 + 0.06 * width) + 2.;
       if (us < best.us) best = {kind, splits, us};
     }
   if (best.kind == 2) {
-    // Every tile of 256 outputs picks its rows again, at a third of the rate of whole boxes: with scratch they are picked once (8192 rows of 4096 -> 16384: 957 us picked
-    // tile by tile, 784 without picking).
-    if (a.rows && a.work && a.o > 1024) {
+    // Every tile of 256 outputs picks its rows again, at a third of the rate of whole boxes: with scratch and many outputs they are picked once (8192 rows of 4096 -> 16384:
+    // 957 us picked tile by tile, 762 picked before; 3800 rows of 16 experts 8192 -> 2048, where the weights of small groups take as long, 170 and 185).
+    if (a.rows && a.work && a.o >= 4096) {
       const tardis_status_t st = launch_gather_rows(a, s);
       if (st != TARDIS_OK) return st;
       a.x = a.work; a.ldx = a.k; a.nx = a.n; a.rows = nullptr;

@@ -424,7 +424,7 @@ LINEAR = dict(n=4, k=64, o=24, dtype=1, out_dtype=1, act=-1, x=1 << 20, ldx=64, 
 
 
 @pytest.mark.parametrize("change", [
-    dict(n=-1), dict(n=1 << 31), dict(k=0), dict(k=60), dict(o=0), dict(dtype=2), dict(dtype=0, out_dtype=1), dict(out_dtype=3), dict(act=3),
+    dict(n=-1), dict(n=(1 << 31) - 4096), dict(k=0), dict(k=(1 << 30) + 8, ldx=1 << 31, ldw=1 << 31), dict(o=(1 << 30) + 1, ldy=1 << 31), dict(k=60), dict(o=0), dict(dtype=2), dict(dtype=0, out_dtype=1), dict(out_dtype=3), dict(act=3),
     dict(act=-2), dict(x=None), dict(W=None), dict(y=None), dict(x=(1 << 20) + 8), dict(W=(1 << 21) + 2), dict(ldx=56), dict(ldx=68),
     dict(ldw=60), dict(ldy=23), dict(y=(1 << 22) + 1), dict(residual=(1 << 23) + 1, ldr=24), dict(residual=1 << 23, ldr=20), dict(bias=(1 << 23) + 2),
     dict(y=(1 << 20) + 16), dict(y=1 << 21), dict(residual=(1 << 22) + 2, ldr=24), dict(residual=1 << 22, ldr=32), dict(y=1 << 22, bias=(1 << 22) + 4),
