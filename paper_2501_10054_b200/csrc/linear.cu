@@ -6,114 +6,153 @@ namespace tardis {
 namespace linear {
 
 // ---- fp32: plain multiply-adds ----
-// 256 threads compute a tile of 16 T outputs x 16 T rows, T x T of them each, over steps of 16 channels in shared memory (channel-major, so that a thread
-// reads its T outputs and its T rows as vectors); the next step's operands are on their way into registers meanwhile.
 template <int T> struct alignas(T > 4 ? 16 : 4 * T) Vec { float v[T]; };
 
-template <int T>
-__global__ void __launch_bounds__(256) k_linear_f32(const __grid_constant__ LinearArgs a) {
-  constexpr int TILE = 16 * T, BK = 16, LD = TILE + 4, PER = TILE * BK / 4 / 256 + (TILE * BK / 4 % 256 != 0);     // PER: 16-byte loads per thread and operand
-  __shared__ __align__(16) float sw[BK][LD], sx[BK][LD];
-  const GroupTile t = find_group_tile(a.offsets, a.groups, a.n, TILE, blockIdx.x);
+// 16 bytes into shared memory, zeros where `there` is false
+__device__ __forceinline__ void copy16(void* dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+
+// 256 threads compute a tile of ROWS x OUTS, a thread 8 x 8 of them (rows ty + TY i, outputs tx + TX j): what bounds this kernel is reading shared memory, 16 multiply-adds
+// per 16-byte read are what it takes to keep up.  (With 4 x 8 per thread 2048 x 1024 x 2048 took 264 us, with packed multiply-adds too, now 224 = 38
+// TFLOP/s; a tile of 32 x 32 with 2 x 2 took 0.6 us for 32 channels.)  Small tiles need fewer threads than that: G groups of them share the channels of a step, and all
+// threads add them up in a fixed order at the end.  Steps of BK channels lie in shared memory as they do in global memory, STAGES - 1 of them on their way (16-byte asynchronous copies).
+template <int ROWS_, int OUTS_, int BK_, int STAGES_> struct CfgF32 {
+  static constexpr int ROWS = ROWS_, OUTS = OUTS_, STAGES = STAGES_, TY = ROWS / 8, TX = OUTS / 8, G = 256 / (TX * TY);
+  static constexpr int BK = BK_, LD = BK + 4, PASS = 1024 / BK /* rows that the threads copy at a time */, STAGE = (ROWS + OUTS) * LD, RING = STAGES * STAGE * 4, SUMS = G > 1 ? G * ROWS * OUTS * 4 : 0;
+  static constexpr int SMEM = RING > SUMS ? RING : SUMS;
+};
+template <typename C>
+__global__ void __launch_bounds__(256, 2) k_linear_f32(const __grid_constant__ LinearArgs a) {
+  constexpr int BK = C::BK, LD = C::LD, STAGES = C::STAGES, XR = C::ROWS / C::PASS, WR = C::OUTS / C::PASS;      // rows of x and of W that a thread copies
+  extern __shared__ __align__(16) float smem_f32[];
+  const GroupTile t = find_group_tile(a.offsets, a.groups, a.n, C::ROWS, blockIdx.x);
   if (t.rows == 0) return;
-  const int o0 = blockIdx.y * TILE, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;      // tx: outputs, ty: rows
-  const float *w[PER], *x[PER];                              // this thread's rows of W and x (null: zeros), four channels at a time
+  const int o0 = blockIdx.y * C::OUTS, k_at = threadIdx.x % (BK / 4) * 4, r_at = threadIdx.x / (BK / 4);
+  const int tx = threadIdx.x % C::TX, ty = threadIdx.x / C::TX % C::TY, g = threadIdx.x / (C::TX * C::TY);
+  int from[XR];                                              // rows of x (-1: zeros)
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int at = threadIdx.x + 256 * i, r = at / (BK / 4);
-    w[i] = x[i] = nullptr;
-    if (at >= TILE * BK / 4) continue;
-    if (o0 + r < a.o) w[i] = static_cast<const float*>(a.W) + t.e * a.stride_w + (o0 + r) * a.ldw + at % (BK / 4) * 4;
-    if (r < t.rows) {
-      const int src = a.rows ? a.rows[t.first + r] : t.first + r;
-      if (src >= 0 && src < a.nx) x[i] = static_cast<const float*>(a.x) + src * a.ldx + at % (BK / 4) * 4;
-    }
+  for (int i = 0; i < XR; ++i) {
+    const int r = r_at + C::PASS * i;
+    from[i] = -1;
+    if (r < t.rows) from[i] = a.rows ? a.rows[t.first + r] : t.first + r;
+    if (from[i] >= a.nx) from[i] = -1;
   }
-  float4 nw[PER], nx[PER];
-  auto load = [&](int k0) {
+  const float* const x_at = static_cast<const float*>(a.x) + k_at;
+  const float* const w_at = static_cast<const float*>(a.W) + t.e * a.stride_w + k_at;
+  const int steps = (a.k + BK - 1) / BK;
+  auto load = [&](int step) {
+    if (step < steps) {
+      float* const to = smem_f32 + step % STAGES * C::STAGE + r_at * LD + k_at;
+      const bool in = step * BK + k_at < a.k;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const bool in = k0 + int(threadIdx.x + 256 * i) % (BK / 4) * 4 < a.k;
-      nw[i] = in && w[i] ? *reinterpret_cast<const float4*>(w[i] + k0) : make_float4(0.f, 0.f, 0.f, 0.f);
-      nx[i] = in && x[i] ? *reinterpret_cast<const float4*>(x[i] + k0) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < XR; ++i) {
+        const bool there = in && from[i] >= 0;
+        copy16(to + C::PASS * i * LD, there ? x_at + from[i] * a.ldx + step * BK : static_cast<const float*>(a.x), there);
+      }
+#pragma unroll
+      for (int i = 0; i < WR; ++i) {
+        const int o = o0 + r_at + C::PASS * i;
+        const bool there = in && o < a.o;
+        copy16(to + (C::ROWS + C::PASS * i) * LD, there ? w_at + o * a.ldw + step * BK : static_cast<const float*>(a.W), there);
+      }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  float acc[T][T] = {};
-  load(0);
-  for (int k0 = 0; k0 < a.k; k0 += BK) {
-    __syncthreads();
+  float acc[8][8] = {};
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int at = threadIdx.x + 256 * i, r = at / (BK / 4), c = at % (BK / 4) * 4;
-      if (at >= TILE * BK / 4) continue;
-      sw[c][r] = nw[i].x; sw[c + 1][r] = nw[i].y; sw[c + 2][r] = nw[i].z; sw[c + 3][r] = nw[i].w;
-      sx[c][r] = nx[i].x; sx[c + 1][r] = nx[i].y; sx[c + 2][r] = nx[i].z; sx[c + 3][r] = nx[i].w;
-    }
-    __syncthreads();
-    if (k0 + BK < a.k) load(k0 + BK);
+  for (int s = 0; s < STAGES - 1; ++s) load(s);
+  for (int step = 0; step < steps; ++step) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+    __syncthreads();                                         // (the stage is there, and nobody still reads the one that is filled next)
+    load(step + STAGES - 1);
+    const float* const sx = smem_f32 + step % STAGES * C::STAGE + ty * LD, *const sw = smem_f32 + step % STAGES * C::STAGE + (C::ROWS + tx) * LD;
+#pragma unroll 1
+    for (int kk = g * 4; kk < BK; kk += C::G * 4) {
+      float4 x[8];
 #pragma unroll
-    for (int kk = 0; kk < BK; ++kk) {
-      const Vec<T> v = *reinterpret_cast<const Vec<T>*>(&sx[kk][ty * T]), u = *reinterpret_cast<const Vec<T>*>(&sw[kk][tx * T]);
+      for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const float4*>(sx + C::TY * i * LD + kk);
 #pragma unroll
-      for (int i = 0; i < T; ++i)
+      for (int j = 0; j < 8; ++j) {
+        const float4 w = *reinterpret_cast<const float4*>(sw + C::TX * j * LD + kk);
 #pragma unroll
-        for (int j = 0; j < T; ++j) acc[i][j] = fmaf(v.v[i], u.v[j], acc[i][j]);
+        for (int i = 0; i < 8; ++i) acc[i][j] = fmaf(x[i].w, w.w, fmaf(x[i].z, w.z, fmaf(x[i].y, w.y, fmaf(x[i].x, w.x, acc[i][j]))));
+      }
     }
   }
-#pragma unroll
-  for (int i = 0; i < T; ++i) {
-    const int r = ty * T + i;
-    if (r >= t.rows) continue;
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  auto finish = [&](int r, int c, float z) {
+    const int o = o0 + c;
+    if (r >= t.rows || o >= a.o) return;
     const long long row = t.first + r;
+    if (a.bias) z += a.bias[(long long)(t.e) * a.o + o];
+    z = apply_act(z, a.act);
+    if (a.res) z += static_cast<const float*>(a.res)[row * a.ldr + o];
+    static_cast<float*>(a.y)[row * a.ldy + o] = z;
+  };
+  if (C::G == 1) {
 #pragma unroll
-    for (int j = 0; j < T; ++j) {
-      const int o = o0 + tx * T + j;
-      if (o >= a.o) continue;
-      float z = acc[i][j];
-      if (a.bias) z += a.bias[(long long)(t.e) * a.o + o];
-      z = apply_act(z, a.act);
-      if (a.res) z += static_cast<const float*>(a.res)[row * a.ldr + o];
-      static_cast<float*>(a.y)[row * a.ldy + o] = z;
-    }
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) finish(ty + C::TY * i, tx + C::TX * j, acc[i][j]);
+    return;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) smem_f32[(g * C::ROWS + ty + C::TY * i) * C::OUTS + tx + C::TX * j] = acc[i][j];
+  __syncthreads();
+#pragma unroll 4
+  for (int at = threadIdx.x; at < C::ROWS * C::OUTS; at += 256) {
+    float z = 0.f;
+#pragma unroll
+    for (int other = 0; other < C::G; ++other) z += smem_f32[other * C::ROWS * C::OUTS + at];
+    finish(at / C::OUTS, at % C::OUTS, z);
   }
 }
 
-template <int T>
-static tardis_status_t launch_f32_tiles(const LinearArgs& a, cudaStream_t s) {
-  const int tile = 16 * T;
-  const long long tiles = (a.n + tile - 1) / tile + (a.offsets ? (a.groups < a.n ? a.groups : a.n) : 0);     // at most
-  const int outputs = (a.o + tile - 1) / tile;
+template <typename C>
+static tardis_status_t launch_f32_tiles(const LinearArgs& a, int dev, cudaStream_t s) {
+  const long long tiles = (a.n + C::ROWS - 1) / C::ROWS + (a.offsets ? (a.groups < a.n ? a.groups : a.n) : 0);     // at most
+  const int outputs = (a.o + C::OUTS - 1) / C::OUTS;
   if (outputs > 65535) return TARDIS_ERR_UNSUPPORTED;
-  k_linear_f32<T><<<dim3(unsigned(tiles), unsigned(outputs)), 256, 0, s>>>(a);
+  static thread_local int room_on = -1;               // the device on which this thread last gave the kernel its shared memory
+  if (dev != room_on) {
+    TARDIS_CUDA_TRY(cudaFuncSetAttribute(k_linear_f32<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+    room_on = dev;
+  }
+  k_linear_f32<C><<<dim3(unsigned(tiles), unsigned(outputs)), 256, C::SMEM, s>>>(a);
   TARDIS_CUDA_TRY(cudaGetLastError());
   return TARDIS_OK;
 }
 
-// Up to eight rows of fp32: a CTA has four outputs, its eight warps share the channels (a lane four at a time) and add their parts in a fixed order.
+// Up to R <= 8 rows of fp32: a CTA has four outputs, its eight warps share the channels (a lane four at a time) and add their parts in a fixed order.
+template <int R>
 __global__ void __launch_bounds__(256) k_linear_few_f32(const __grid_constant__ LinearArgs a) {
-  constexpr int O = 4, ROWS = 8;
-  __shared__ float part[8][O * ROWS];
-  const GroupTile t = find_group_tile(a.offsets, a.groups, a.n, ROWS, blockIdx.y);
+  constexpr int O = 4;
+  __shared__ float part[8][O * R];
+  const GroupTile t = find_group_tile(a.offsets, a.groups, a.n, R, blockIdx.y);
   if (t.rows == 0) return;
   const int o0 = blockIdx.x * O, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const float *w[O], *x[ROWS];
+  const float *w[O], *x[R];
 #pragma unroll
   for (int i = 0; i < O; ++i) w[i] = static_cast<const float*>(a.W) + t.e * a.stride_w + min(o0 + i, a.o - 1) * a.ldw;
-  bool there[ROWS];
+  bool there[R];
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
+  for (int r = 0; r < R; ++r) {
     int src = -1;
     if (r < t.rows) src = a.rows ? a.rows[t.first + r] : t.first + r;
     there[r] = src >= 0 && src < a.nx;
     x[r] = static_cast<const float*>(a.x) + (there[r] ? src : 0) * a.ldx;
   }
-  float acc[O][ROWS] = {};
+  float acc[O][R] = {};
   for (int k = threadIdx.x * 4; k < a.k; k += 1024) {
     float4 wv[O];
 #pragma unroll
     for (int i = 0; i < O; ++i) wv[i] = *reinterpret_cast<const float4*>(w[i] + k);
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
+    for (int r = 0; r < R; ++r) {
       if (!there[r]) continue;
       const float4 xv = *reinterpret_cast<const float4*>(x[r] + k);
 #pragma unroll
@@ -123,7 +162,7 @@ __global__ void __launch_bounds__(256) k_linear_few_f32(const __grid_constant__ 
 #pragma unroll
   for (int i = 0; i < O; ++i)
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
+    for (int r = 0; r < R; ++r) {
       float v = acc[i][r];
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
@@ -131,7 +170,7 @@ __global__ void __launch_bounds__(256) k_linear_few_f32(const __grid_constant__ 
     }
   __syncthreads();
   const int r = threadIdx.x / O, o = o0 + threadIdx.x % O;
-  if (threadIdx.x >= O * ROWS || r >= t.rows || o >= a.o) return;
+  if (threadIdx.x >= O * R || r >= t.rows || o >= a.o) return;
   float z = 0.f;
   for (int i = 0; i < 8; ++i) z += part[i][threadIdx.x];
   const long long row = t.first + r;
@@ -143,16 +182,23 @@ __global__ void __launch_bounds__(256) k_linear_few_f32(const __grid_constant__ 
 
 static tardis_status_t launch_f32(const LinearArgs& a, cudaStream_t s) {
   if (a.n <= 8) {
-    const unsigned tiles = a.offsets ? unsigned(a.n) : 1u;                             // at most (a group's tile has a row)
-    k_linear_few_f32<<<dim3(unsigned((a.o + 3) / 4), tiles), 256, 0, s>>>(a);
+    const dim3 grid(unsigned((a.o + 3) / 4), a.offsets ? unsigned(a.n) : 1u);          // at most (a group's tile has a row)
+    if (a.n == 1) k_linear_few_f32<1><<<grid, 256, 0, s>>>(a);
+    else if (a.n <= 3) k_linear_few_f32<3><<<grid, 256, 0, s>>>(a);
+    else k_linear_few_f32<8><<<grid, 256, 0, s>>>(a);
     TARDIS_CUDA_TRY(cudaGetLastError());
     return TARDIS_OK;
   }
-  // the largest tiles that give every SM one: few rows and outputs are all latency
+  int dev = 0, sms = 0;
+  TARDIS_CUDA_TRY(cudaGetDevice(&dev));
+  TARDIS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  // The largest tiles that keep the SMs busy (a tile's time hardly depends on how many there are; us with tiles of 128 x 128, 64 x 64, 32 x 64, 16 x 32: 2048 x 64 x
+  // 2048 26 / 34 / 46 / 178, 1024 x 256 x 1024 42 / 24 / 28 / 56, 256 x 256 x 1024 42 / 15 / 9.6 / 17, 64 x 256 x 1024 37 / 14 / 9 / 5.7).
   const long long groups = a.offsets ? a.groups : 1, rows = (a.n + groups - 1) / groups;
-  auto tiles = [&](int tile) { return (a.o + tile - 1) / tile * (groups * ((rows + tile - 1) / tile)); };
-  if (tiles(128) >= 148) return launch_f32_tiles<8>(a, s);
-  return tiles(64) >= 148 ? launch_f32_tiles<4>(a, s) : launch_f32_tiles<2>(a, s);
+  auto tiles = [&](int high, int wide) { return (a.o + wide - 1) / wide * (groups * ((rows + high - 1) / high)); };
+  if (tiles(128, 128) * 10 >= sms * 13) return launch_f32_tiles<CfgF32<128, 128, 32, 3>>(a, dev, s);
+  if (tiles(64, 64) * 10 >= sms * 15) return launch_f32_tiles<CfgF32<64, 64, 32, 4>>(a, dev, s);
+  return tiles(32, 64) * 10 >= sms * 6 ? launch_f32_tiles<CfgF32<32, 64, 32, 6>>(a, dev, s) : launch_f32_tiles<CfgF32<16, 32, 128, 3>>(a, dev, s);
 }
 
 // ---- up to eight rows of bf16: bound by reading the weights once ----
