@@ -214,7 +214,7 @@ def test_grouped_matches_definition(sizes, k, o, dtype):
 
 
 @gpu
-@pytest.mark.parametrize("sizes,k,o", [([700, 1500, 0, 4000], 2048, 1024), ([90] * 16, 1024, 2048), ([1, 0, 1, 2], 4096, 4544), ([1400, 30, 2], 4544, 520),
+@pytest.mark.parametrize("sizes,k,o", [([700, 1500, 0, 4000], 2048, 1024), ([300, 1800, 0, 401], 264, 4200), ([90] * 16, 1024, 2048), ([1, 0, 1, 2], 4096, 4544), ([1400, 30, 2], 4544, 520),
                                        ([9, 0, 14, 25, 3, 0, 1, 44], 4096, 1024)])
 def test_grouped_large(sizes, k, o):
     test_grouped_matches_definition(sizes, k, o, BF)
