@@ -229,6 +229,14 @@ def _raw_stream(stream, index: int) -> int:
     return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
 
 
+def _empty(x: torch.Tensor, shape, dtype, stream) -> torch.Tensor:
+    """Memory for a call on `stream`: taken from that stream's own, which nothing that is still under way on the current one uses."""
+    if stream is None:
+        return x.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return x.new_empty(shape, dtype=dtype)
+
+
 def tardis_linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = TARDIS_ACT_NONE,
                   residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype=None, stream=None):
     """y = act(x W^T + bias) + residual in one launch (see tardis_linear in tardis.h): x [n, k], W [o, k] float32 or bfloat16
@@ -242,7 +250,7 @@ def tardis_linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor]
         out_dtype = dtype if out is None else out.dtype
     code, out_code = _dtype_code(dtype), _dtype_code(out_dtype)
     if out is None:
-        out = x.new_empty((n, o), dtype=out_dtype)
+        out = _empty(x, (n, o), out_dtype, stream)
     px, ldx = _matrix(x, "x", dtype, n, k, index)
     pw, ldw = _matrix(W, "W", dtype, o, k, index)
     py, ldy = _matrix(out, "out", out_dtype, n, o, index)
@@ -273,15 +281,15 @@ def _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, back, wor
         ps, pc = _vector(slots, "slots", i32, (tokens, top_k), index), _vector(weights, "weights", torch.float32, (tokens, top_k), index)
         n_out, room = tokens, 4 * n * o
         if work is None:
-            work = x.new_empty((n * o,), dtype=torch.float32)
+            work = _empty(x, (n * o,), torch.float32, stream)
         elif work.get_device() != index or not work.is_contiguous() or work.numel() * work.element_size() < room:
             raise TardisError(1, "work must be a contiguous tensor of at least 4 rows o bytes on x's device")
         pwork = work.data_ptr()
-    elif rows is not None and n >= 1024 and dtype is torch.bfloat16:
-        work, room = x.new_empty((n, k)), 2 * n * k
+    elif rows is not None and n >= 1024 and o >= 4096 and dtype is torch.bfloat16:       # (where long calls use it)
+        work, room = _empty(x, (n, k), dtype, stream), 2 * n * k
         pwork = work.data_ptr()
     if out is None:
-        out = x.new_empty((n_out, o), dtype=out_dtype)
+        out = _empty(x, (n_out, o), out_dtype, stream)
     px, ldx = _matrix(x, "x", dtype, nx, k, index)
     stride_w, ldw, unit = W.stride()
     if W.dtype is not dtype or W.get_device() != index or unit != 1:
@@ -328,10 +336,10 @@ def tardis_route(logits: torch.Tensor, top_k: int, normalise: bool = True, strea
     if not 1 <= top_k <= e:
         raise TardisError(1, "top_k must be between 1 and the number of experts")
     i32 = torch.int32
-    experts, slots, rows, weights = logits.new_empty((4, n, top_k), dtype=i32).unbind(0)       # (one allocation)
+    experts, slots, rows, weights = _empty(logits, (4, n, top_k), i32, stream).unbind(0)       # (one allocation)
     rows, weights = rows.view(-1), weights.view(torch.float32)
-    offsets = logits.new_empty((e + 1,), dtype=i32)
-    work = logits.new_empty((1024 * e,), dtype=i32) if n > 128 else None
+    offsets = _empty(logits, (e + 1,), i32, stream)
+    work = _empty(logits, (1024 * e,), i32, stream) if n > 128 else None
     status = load_library().tardis_route(n, e, top_k, 1 if normalise else 0, pl, ldl, experts.data_ptr(), weights.data_ptr(),
                                          offsets.data_ptr(), rows.data_ptr(), slots.data_ptr(), work.data_ptr() if work is not None else 0,
                                          4096 * e if work is not None else 0, _raw_stream(stream, index))

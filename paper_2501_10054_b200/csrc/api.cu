@@ -356,7 +356,7 @@ static bool linear_args_ok(const LinearArgs& a, long long n, long long nx, long 
   return a.ldx <= kMostLd && a.ldw <= kMostLd && a.ldy <= kMostLd && (!a.res || a.ldr <= kMostLd) && a.stride_w <= kMostLd;
 }
 static bool linear_pointers_ok(const LinearArgs& a, long long nx, long long out_rows) {
-  if (!a.x || !a.W || !a.y || !aligned16(a.x) || !aligned16(a.W)) return false;
+  if (!a.y || (a.n > 0 && (!a.x || !a.W)) || !aligned16(a.x) || !aligned16(a.W)) return false;
   const long long in = a.dtype == TARDIS_BF16 ? 2 : 4, out = a.out_dtype == TARDIS_BF16 ? 2 : 4;
   auto off = [](const void* p, long long unit) { return (reinterpret_cast<uintptr_t>(p) & (unit - 1)) != 0; };
   if (off(a.y, out) || off(a.res, out) || off(a.bias, 4)) return false;
@@ -402,7 +402,7 @@ tardis_status_t tardis_grouped_linear(const tardis_grouped_desc_t* d, tardis_str
   if (a.groups > 1 && (a.stride_w % 8 || a.stride_w < (a.o - 1) * a.ldw + a.k)) return TARDIS_ERR_INVALID_ARG;
   if (back && (!d->slots || !d->weights || d->top_k <= 0)) return TARDIS_ERR_INVALID_ARG;
   if (out_rows == 0) return TARDIS_OK;
-  if (!a.offsets || d->n_x < (a.rows ? 1 : d->n_rows) || (reinterpret_cast<uintptr_t>(a.offsets) | reinterpret_cast<uintptr_t>(a.rows)) & 3u) return TARDIS_ERR_INVALID_ARG;
+  if (!a.offsets || (d->n_rows > 0 && d->n_x < (a.rows ? 1 : d->n_rows)) || (reinterpret_cast<uintptr_t>(a.offsets) | reinterpret_cast<uintptr_t>(a.rows)) & 3u) return TARDIS_ERR_INVALID_ARG;
   if (!linear_pointers_ok(a, d->n_x, out_rows)) return TARDIS_ERR_INVALID_ARG;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (!back) {

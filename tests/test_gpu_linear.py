@@ -241,6 +241,70 @@ def test_grouped_whatever_offsets_and_rows_hold(n):
 
 
 @gpu
+@pytest.mark.parametrize("sizes_at,n", [({3: 2, 1000: 1, 1023: 3}, 6), ({0: 40, 511: 1, 512: 300, 1023: 20}, 361)])
+def test_grouped_with_1024_experts(sizes_at, n):
+    k, o = 64, 24
+    x, W, b, _ = make(n, k, o, BF, groups=1024)
+    for dtype in (BF, F32):
+        xd, Wd = x.to(dtype), W.to(dtype)
+        y = T.tardis_grouped_linear(xd, Wd, offsets_of([sizes_at.get(e, 0) for e in range(1024)]), bias=b)
+        at = 0
+        for e, size in sorted(sizes_at.items()):
+            check(y[at:at + size], *product64(xd[at:at + size], Wd[e], b[e], NONE))
+            at += size
+
+
+@gpu
+def test_grouped_gathers_once_whatever_offsets_hold():
+    """The long form with scratch: offsets that fall again still leave the rows in front of the fall in their groups."""
+    n, k, o = 2048, 72, 4104
+    x, W, b, _ = make(n, k, o, BF, groups=3)
+    rows = torch.randperm(n, device="cuda").int()
+    rows[5], rows[1900] = -3, n
+    xs = x[rows.long().clamp(0, n - 1)].clone()
+    xs[5] = xs[1900] = 0
+    y = torch.full((n, o), 7.0, dtype=BF, device="cuda")
+    T.tardis_grouped_linear(x, W, torch.tensor([1, 1000, 2000, 30], dtype=torch.int32, device="cuda"), bias=b, rows=rows, out=y)
+    check(y[1:1000], *product64(xs[1:1000], W[0], b[0], NONE))
+    check(y[1000:2000], *product64(xs[1000:2000], W[1], b[1], NONE))
+    assert (y[0] == 7).all() and (y[2000:] == 7).all()
+
+
+@gpu
+def test_combine_without_rows_and_without_tokens():
+    W, r = torch.randn(2, 24, 64, device="cuda").bfloat16(), torch.randn(3, 24, device="cuda").bfloat16()
+    off, slots, w = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.full((3, 2), -1, dtype=torch.int32, device="cuda"), torch.zeros(3, 2, device="cuda")
+    y = T.tardis_grouped_linear_combine(W.new_empty(0, 64), W, off, slots, w, residual=r)
+    assert torch.equal(y, r)
+    assert T.tardis_grouped_linear_combine(W.new_empty(0, 64), W, off, slots[:0], w[:0]).shape == (0, 24)
+    assert T.tardis_grouped_linear(W.new_empty(0, 64), W, off).shape == (0, 24)
+    assert T.tardis_linear(W.new_empty(0, 64), W[0]).shape == (0, 24)
+
+
+@gpu
+def test_calls_on_another_stream_use_its_memory():
+    """Results and scratch made for a call on a given stream, while the current stream is busy with memory that it has given back."""
+    s = torch.cuda.Stream()
+    tokens, experts, k, o = 3000, 8, 64, 4104
+    logits = torch.randn(tokens, experts, device="cuda")
+    x, W, b, _ = make(tokens, k, o, BF, groups=experts)
+    want_route = T.tardis_route(logits, 2)
+    want = T.tardis_grouped_linear(x, W, want_route[2], bias=b, rows=want_route[3])
+    _, W2, _, _ = make(1, o, 72, BF, groups=experts)
+    want_back = T.tardis_grouped_linear_combine(want, W2, want_route[2], want_route[4], want_route[1])
+    torch.cuda.synchronize()
+    a = torch.randn(4096, 4096, device="cuda")
+    for _ in range(3):
+        for _ in range(10):
+            a @ a                                              # its result goes back to the current stream's memory at once
+        route = T.tardis_route(logits, 2, stream=s)
+        y = T.tardis_grouped_linear(x, W, route[2], bias=b, rows=route[3], stream=s)
+        back = T.tardis_grouped_linear_combine(y, W2, route[2], route[4], route[1], stream=s)
+        s.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(route, want_route)) and torch.equal(y, want) and torch.equal(back, want_back)
+
+
+@gpu
 def test_grouped_strided_weights_and_outputs():
     for n in (5, 50, 300):
         x, _, b, _ = make(n, 136, 65, BF, groups=3)
@@ -276,13 +340,14 @@ def test_combine_matches_definition(tokens, experts, top_k, k, o, dtype):
     f = torch.zeros(n, o, dtype=torch.float64, device="cuda")
     tol = torch.zeros_like(f)
     ends = off.tolist()
+    act = TANH if tokens % 2 else NONE
     for e in range(experts):
         own = slice(ends[e], ends[e + 1])
-        f[own], tol[own] = product64(x[own], W[e], b[e], NONE)
+        f[own], tol[own] = product64(x[own], W[e], b[e], act)
     x[ends[-1]:] = float("nan")
     for res in (None, r):
         work = torch.full((n, o), float("nan"), device="cuda")
-        y = T.tardis_grouped_linear_combine(x, W, off, slots, w, bias=b, residual=res, work=work)
+        y = T.tardis_grouped_linear_combine(x, W, off, slots, w, bias=b, act=act, residual=res, work=work)
         there = (slots >= 0)[:, :, None]
         pick = slots.long().clamp(min=0)
         ref = torch.where(there, f[pick] * w.double()[:, :, None], 0.0)
