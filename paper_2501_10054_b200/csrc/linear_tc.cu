@@ -7,7 +7,7 @@
 // or 128 bytes.
 //
 // A CTA is persistent: warp 0 stages 128 x 64 (weights) and up to NT x 64 (tokens) boxes with TMA (128-byte swizzle, no multicast), the tokens as boxes
-// of 32 rows or, where the rows of a group are picked by an index array, four rows at a time by their indices (tile::gather4); warp 1 issues the MMAs into
+// of 32 rows or, where the rows of a group are picked by an index array, four rows at a time by their indices (tile::gather4, four more warps); warp 1 issues the MMAs into
 // one of two accumulators; warps 2 .. 9 run the epilogue of the other.  CTAS = 2: two CTAs share a tile of 256 channels, each with 128 of them and half of
 // the tokens in shared memory (cta_group::2).  SPLIT: the CTAs of a cluster share the channels k of a tile; each hands the others the columns that
 // they finish through their shared memory, and the owner of a column adds the parts in the order of their ranks: no atomics, no scratch, the same bits
@@ -214,17 +214,6 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     if (CTAS == 2) tmem_alloc_pair(tmem_slot, C::TMEM_COLS);
     else tmem_alloc(tmem_slot, C::TMEM_COLS);
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");             // (x, offsets, ... may come from the launch before)
-  int ntiles;
-  if (a.offsets) build_groups(a.offsets, a.groups, a.n, NT, mt, groups);
-  tc_fence_before();
-  __syncthreads();
-  if (in_cluster > 1) cluster_sync();                            // (the other CTAs' barriers are reported to)
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (this CTA has its tensor memory)
-  tc_fence_after();
-  const uint32_t tmem_base = *tmem_slot;
-  ntiles = a.offsets ? groups.firsts[a.groups] : (a.n + NT - 1) / NT * mt;
-
   // this CTA's part of the k blocks
   const int per_split = SPLIT ? (p.kblocks + SPLITS - 1) / SPLITS : p.kblocks;
   const int kb_lo = SPLIT ? min(rank * per_split, p.kblocks) : 0, nkb = SPLIT ? min(p.kblocks, kb_lo + per_split) - kb_lo : p.kblocks;
@@ -257,6 +246,24 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     t.nt = max(C::STEP, (t.rows + C::STEP - 1) & ~(C::STEP - 1));
     return t;
   };
+  if (CTAS == 1 && !SPLIT && !a.offsets && warp == 0 && first_tile < (a.n + NT - 1) / NT * mt) {
+    // while the launch before ends: the first weights on their way into L2 (64 tokens of 4096 -> 16384 25.5 -> 24.9 us; clusters gained nothing)
+    const Tile t = decode(first_tile);
+    if (elect_one())
+      for (int kb = 0; kb < min(nkb, C::NS); ++kb)
+        asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(&tmW), "r"((kb_lo + (kb + t.turn) % nkb) * BK), "r"(t.o0), "r"(0) : "memory");
+    __syncwarp();
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");             // (x, offsets, ... may come from the launch before)
+  if (a.offsets) build_groups(a.offsets, a.groups, a.n, NT, mt, groups);
+  tc_fence_before();
+  __syncthreads();
+  if (in_cluster > 1) cluster_sync();                            // (the other CTAs' barriers are reported to)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (this CTA has its tensor memory)
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int ntiles = a.offsets ? groups.firsts[a.groups] : (a.n + NT - 1) / NT * mt;
+
   int issued = 0;
   if (warp == 0) {
     // ---------------- copies ----------------
@@ -323,6 +330,8 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   } else if (GATHER && warp >= NTHREADS / 32) {
     // ---------------- rows of x by their indices ----------------
     // Each of four warps has a quarter of this CTA's rows, their indices in registers that all lanes hold alike, and copies them four at a time.
+    // (8192 rows of 8 experts, 4096 -> 16384: 898 us; issued by the 32 lanes of one warp 2490, 80 cycles each; copied by threads, whose writes need a fence towards the
+    // tensor cores, 2040.)
     constexpr int QUADS = C::B_ROWS / (4 * GATHER_WARPS);
     const int w = warp - NTHREADS / 32;
     int s = 0, parity = 1;
