@@ -279,11 +279,11 @@ def _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, back, wor
             raise TardisError(1, "slots must be [tokens, top_k]")
         tokens, top_k = slots.shape
         ps, pc = _vector(slots, "slots", i32, (tokens, top_k), index), _vector(weights, "weights", torch.float32, (tokens, top_k), index)
-        n_out, room = tokens, 4 * n * o
+        n_out, room = tokens, 4 * n * ((o + 7) // 8 * 8)
         if work is None:
-            work = _empty(x, (n * o,), torch.float32, stream)
+            work = _empty(x, (room // 4,), torch.float32, stream)
         elif work.get_device() != index or not work.is_contiguous() or work.numel() * work.element_size() < room:
-            raise TardisError(1, "work must be a contiguous tensor of at least 4 rows o bytes on x's device")
+            raise TardisError(1, "work must be a contiguous tensor of at least 4 rows o bytes (o rounded up to 8) on x's device")
         pwork = work.data_ptr()
     elif rows is not None and n >= 1024 and o >= 4096 and dtype is torch.bfloat16:       # (where long calls use it)
         work, room = _empty(x, (n, k), dtype, stream), 2 * n * k
@@ -319,7 +319,7 @@ def tardis_grouped_linear_combine(x: torch.Tensor, W: torch.Tensor, offsets: tor
                                   residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype=None,
                                   work: Optional[torch.Tensor] = None, stream=None):
     """tardis_grouped_linear and the weighted return to the tokens: y[t] = residual[t] + sum_c weights[t, c] f[slots[t, c]], slots int32
-    and weights float32 [tokens, top_k].  `work` is scratch of 4 rows o bytes (made here when not given)."""
+    and weights float32 [tokens, top_k].  `work` is scratch of 4 rows o bytes, o rounded up to a multiple of 8 (made here when not given)."""
     return _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, (slots, weights), work, stream,
                     "tardis_grouped_linear_combine")
 

@@ -411,15 +411,16 @@ tardis_status_t tardis_grouped_linear(const tardis_grouped_desc_t* d, tardis_str
     return launch_linear(a, s);
   }
   if ((reinterpret_cast<uintptr_t>(d->slots) | reinterpret_cast<uintptr_t>(d->weights)) & 3u) return TARDIS_ERR_INVALID_ARG;
-  const size_t room = size_t(a.n) * size_t(a.o) * 4;
+  const int ldf = (a.o + 7) & ~7;                            // (so that rows are aligned whatever o is)
+  const size_t room = size_t(a.n) * size_t(ldf) * 4;
   if (room > 0 && (!d->work || !aligned16(d->work) || d->work_bytes < room)) return TARDIS_ERR_INVALID_ARG;
   LinearArgs f = a;
-  f.res = nullptr; f.y = d->work; f.ldy = a.o; f.out_dtype = TARDIS_F32;
+  f.res = nullptr; f.y = d->work; f.ldy = ldf; f.out_dtype = TARDIS_F32;
   if (f.n > 0) {
     const tardis_status_t st = launch_linear(f, s);
     if (st != TARDIS_OK) return st;
   }
-  return launch_combine(int(out_rows), d->top_k, a, static_cast<const float*>(d->work), d->slots, d->weights, s);
+  return launch_combine(int(out_rows), d->top_k, a, static_cast<const float*>(d->work), ldf, d->slots, d->weights, s);
 }
 
 tardis_status_t tardis_route(int64_t n_tokens, int32_t n_experts, int32_t top_k, int32_t normalise, const float* logits, int64_t ldl,

@@ -6,8 +6,6 @@ namespace tardis {
 namespace linear {
 
 // ---- fp32: plain multiply-adds ----
-template <int T> struct alignas(T > 4 ? 16 : 4 * T) Vec { float v[T]; };
-
 // 16 bytes into shared memory, zeros where `there` is false
 __device__ __forceinline__ void copy16(void* dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -341,66 +339,75 @@ static tardis_status_t launch_few(const LinearArgs& a, cudaStream_t s) {
 }
 
 // ---- the return to the tokens: bound by reading f ----
-// A thread adds up V outputs of a token, its choices in their order (four loads of f under way at a time).
-template <int V, typename O>
-__global__ void __launch_bounds__(256) k_combine(const __grid_constant__ LinearArgs a, int top_k, const float* __restrict__ f,
-                                                 const int* __restrict__ slots, const float* __restrict__ weights) {
+// A thread adds up four outputs of a token, its choices in their order (four loads of f under way at a time).  wide: y and the residual are touched four at a time too.
+template <typename O>
+__global__ void __launch_bounds__(256) k_combine(const __grid_constant__ LinearArgs a, int top_k, const float* __restrict__ f, int ldf,
+                                                 const int* __restrict__ slots, const float* __restrict__ weights, int wide) {
+  struct alignas(4 * sizeof(O)) Out { O v[4]; };
   const long long t = blockIdx.x;
-  const int c = (blockIdx.y * 256 + threadIdx.x) * V;
+  const int c = (blockIdx.y * 256 + threadIdx.x) * 4;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (c >= a.o) return;
-  const int lo = max(a.offsets[0], 0), hi = min(a.offsets[a.groups], a.n);
-  Vec<V> sum = {};
-  struct alignas(sizeof(O) * V) Out { O v[V]; };
+  const int lo = max(a.offsets[0], 0), hi = min(a.offsets[a.groups], a.n), count = min(4, a.o - c);
+  const O* const res = static_cast<const O*>(a.res) + t * a.ldr + c;
+  O* const to = static_cast<O*>(a.y) + t * a.ldy + c;
+  float sum[4] = {};
   Out old;
-  if (a.res) old = *reinterpret_cast<const Out*>(static_cast<const O*>(a.res) + t * a.ldr + c);
+  if (a.res) {
+    if (wide) old = *reinterpret_cast<const Out*>(res);
+    else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) old.v[i] = i < count ? res[i] : from_f32<O>(0.f);
+    }
+  }
   for (int j0 = 0; j0 < top_k; j0 += 4) {
-    Vec<V> part[4];
+    float4 part[4];
     float w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int slot = j0 + j < top_k ? slots[t * top_k + j0 + j] : -1;
       const bool there = slot >= lo && slot < hi;
       w[j] = there ? weights[t * top_k + j0 + j] : 0.f;
-      part[j] = there ? *reinterpret_cast<const Vec<V>*>(f + (long long)(slot) * a.o + c) : Vec<V>{};
+      part[j] = there ? *reinterpret_cast<const float4*>(f + (long long)(slot) * ldf + c) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < V; ++i) sum.v[i] = fmaf(w[j], part[j].v[i], sum.v[i]);
+    for (int j = 0; j < 4; ++j) {
+      sum[0] = fmaf(w[j], part[j].x, sum[0]);
+      sum[1] = fmaf(w[j], part[j].y, sum[1]);
+      sum[2] = fmaf(w[j], part[j].z, sum[2]);
+      sum[3] = fmaf(w[j], part[j].w, sum[3]);
+    }
   }
   Out y;
 #pragma unroll
-  for (int i = 0; i < V; ++i) y.v[i] = from_f32<O>(a.res ? sum.v[i] + to_f32(old.v[i]) : sum.v[i]);
-  *reinterpret_cast<Out*>(static_cast<O*>(a.y) + t * a.ldy + c) = y;
-}
-
-template <int V, typename O>
-static tardis_status_t launch_combine_as(int tokens, int top_k, const LinearArgs& a, const float* f, const int* slots, const float* weights,
-                                         cudaStream_t s) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(tokens), unsigned((a.o + 256 * V - 1) / (256 * V))); cfg.blockDim = dim3(256); cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr; cfg.numAttrs = 1;
-  TARDIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_combine<V, O>, a, top_k, f, slots, weights));
-  return TARDIS_OK;
+  for (int i = 0; i < 4; ++i) y.v[i] = from_f32<O>(a.res ? sum[i] + to_f32(old.v[i]) : sum[i]);
+  if (wide) *reinterpret_cast<Out*>(to) = y;
+  else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < count) to[i] = y.v[i];
+  }
 }
 
 }  // namespace linear
 
-tardis_status_t launch_combine(int tokens, int top_k, const LinearArgs& a, const float* f, const int* slots, const float* weights,
+tardis_status_t launch_combine(int tokens, int top_k, const LinearArgs& a, const float* f, int ldf, const int* slots, const float* weights,
                                cudaStream_t s) {
   using namespace linear;
   const size_t unit = a.out_dtype == TARDIS_BF16 ? 2 : 4;
   auto fits = [&](const void* p, long long ld) { return !p || ((reinterpret_cast<uintptr_t>(p) | size_t(ld) * unit) & (4 * unit - 1)) == 0; };
-  const bool wide = a.o % 4 == 0 && fits(a.y, a.ldy) && fits(a.res, a.ldr);        // four outputs at a time
-  if (a.o > 65535 * 256) return TARDIS_ERR_UNSUPPORTED;
-  if (a.out_dtype == TARDIS_BF16)
-    return wide ? launch_combine_as<4, __nv_bfloat16>(tokens, top_k, a, f, slots, weights, s) : launch_combine_as<1, __nv_bfloat16>(tokens, top_k, a, f, slots, weights, s);
-  return wide ? launch_combine_as<4, float>(tokens, top_k, a, f, slots, weights, s) : launch_combine_as<1, float>(tokens, top_k, a, f, slots, weights, s);
+  const int wide = a.o % 4 == 0 && fits(a.y, a.ldy) && fits(a.res, a.ldr);
+  if ((a.o + 1023) / 1024 > 65535) return TARDIS_ERR_UNSUPPORTED;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(tokens), unsigned((a.o + 1023) / 1024)); cfg.blockDim = dim3(256); cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  TARDIS_CUDA_TRY(a.out_dtype == TARDIS_BF16 ? cudaLaunchKernelEx(&cfg, k_combine<__nv_bfloat16>, a, top_k, f, ldf, slots, weights, wide)
+                                             : cudaLaunchKernelEx(&cfg, k_combine<float>, a, top_k, f, ldf, slots, weights, wide));
+  return TARDIS_OK;
 }
 
 tardis_status_t launch_linear(const LinearArgs& a, cudaStream_t s) {

@@ -25,9 +25,9 @@ struct LinearArgs {
 
 tardis_status_t launch_linear(const LinearArgs& a, cudaStream_t s);
 tardis_status_t launch_linear_tc(const LinearArgs& a, cudaStream_t s);       // bf16, n > 0
-// What a gives in fp32 as f [a.n, a.o], returned to the tokens: a.y[t, o] = a.res[t, o] + sum_j weights[t, j] f[slots[t, j], o]; slots outside
+// What a gives in fp32 as f [a.n, a.o] (rows of ldf, a multiple of 4), returned to the tokens: a.y[t, o] = a.res[t, o] + sum_j weights[t, j] f[slots[t, j], o]; slots outside
 // the groups add nothing
-tardis_status_t launch_combine(int tokens, int top_k, const LinearArgs& a, const float* f, const int* slots, const float* weights,
+tardis_status_t launch_combine(int tokens, int top_k, const LinearArgs& a, const float* f, int ldf, const int* slots, const float* weights,
                                cudaStream_t s);
 tardis_status_t launch_route(int tokens, int experts, int top_k, int normalise, const float* logits, long long ldl, int* chosen,
                              float* weights, int* offsets, int* rows, int* slots, int* work, cudaStream_t s);

@@ -346,7 +346,7 @@ def test_combine_matches_definition(tokens, experts, top_k, k, o, dtype):
         f[own], tol[own] = product64(x[own], W[e], b[e], act)
     x[ends[-1]:] = float("nan")
     for res in (None, r):
-        work = torch.full((n, o), float("nan"), device="cuda")
+        work = torch.full((n, (o + 7) // 8 * 8), float("nan"), device="cuda")
         y = T.tardis_grouped_linear_combine(x, W, off, slots, w, bias=b, act=act, residual=res, work=work)
         there = (slots >= 0)[:, :, None]
         pick = slots.long().clamp(min=0)
