@@ -104,21 +104,42 @@ template <int ACT, typename O> __device__ __forceinline__ float activation(float
 
 // The epilogue takes sixteen columns of a warp's 32 channels o0 .. o0 + 31 at a time through shared memory (`stage`, column-major), `count` of them rows of y
 // from `row` on.  Where y and the residual are aligned and all channels are inside, a lane has 8 channels of a token and touches both 16 bytes at a
-// time, the residual of the next sixteen columns on its way; else its own channel of one token after the other.  (Two bytes per lane throughout: the
-// epilogue of 1024 x 64 x 16384 with a residual took 51 us, with the residual read when it is needed 35.)
-template <typename O> struct Eight { uint4 piece[sizeof(O) / 2]; };
+// time; else its own channel of all sixteen tokens.  The residual of the next sixteen columns is on its way meanwhile.  (Two bytes per lane throughout: the
+// epilogue of 1024 x 64 x 16384 with a residual took 51 us, with the residual read when it is needed 35, so 30.)
 template <typename O> struct alignas(16) Out8 { O v[8]; };
+// Sixteen residuals as words, packed as they lie in memory (wide: eight of token c, eight of c + 8) or one each (one of every token: packing them would wait
+// for each in turn)
+template <typename O> struct Old {
+  uint32_t w[16];
+  __device__ __forceinline__ float packed(int i) const {
+    return __uint_as_float(sizeof(O) == 4 ? w[i] : i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+  __device__ __forceinline__ float one(int i) const { return __uint_as_float(sizeof(O) == 4 ? w[i] : w[i] << 16); }
+};
 template <typename O>
-__device__ __forceinline__ void read_residual(const LinearArgs& a, long long row, int count, int o0, int lane, Eight<O> (&old)[2]) {
+__device__ __forceinline__ void read_residual(const LinearArgs& a, bool wide, long long row, int count, int o0, int lane, Old<O>& old) {
+  constexpr int HALF = 2 * sizeof(O);                          // words of eight
+  if (wide) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int i = 0; i < int(sizeof(O) / 2); ++i)
-      if (h * 8 + (lane >> 2) < count)
-        old[h].piece[i] = reinterpret_cast<const uint4*>(static_cast<const O*>(a.res) + (row + h * 8 + (lane >> 2)) * a.ldr + o0 + (lane & 3) * 8)[i];
+      for (int i = 0; i < HALF; i += 4)
+        if (h * 8 + (lane >> 2) < count) {
+          const uint4 v = reinterpret_cast<const uint4*>(static_cast<const O*>(a.res) + (row + h * 8 + (lane >> 2)) * a.ldr + o0 + (lane & 3) * 8)[i / 4];
+          old.w[h * HALF + i] = v.x; old.w[h * HALF + i + 1] = v.y; old.w[h * HALF + i + 2] = v.z; old.w[h * HALF + i + 3] = v.w;
+        }
+  } else {
+    const O* const r = static_cast<const O*>(a.res) + row * a.ldr + o0 + lane;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const bool there = i < count && o0 + lane < a.o;
+      if (sizeof(O) == 4) old.w[i] = there ? *reinterpret_cast<const uint32_t*>(r + i * a.ldr) : 0u;
+      else old.w[i] = there ? *reinterpret_cast<const unsigned short*>(r + i * a.ldr) : 0u;
+    }
+  }
 }
 template <int ACT, typename O>
-__device__ __forceinline__ void finish(const LinearArgs& a, bool wide, long long row, int count, int o0, const float* stage, int lane, const Eight<O> (&old)[2]) {
+__device__ __forceinline__ void finish(const LinearArgs& a, bool wide, long long row, int count, int o0, const float* stage, int lane, const Old<O>& old) {
   if (wide) {
     const int c = lane >> 2, ch = (lane & 3) * 8;                // this lane's column of 8 and its channels
 #pragma unroll
@@ -132,19 +153,19 @@ __device__ __forceinline__ void finish(const LinearArgs& a, bool wide, long long
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float v = activation<ACT, O>(z[i]);
-        if (a.res) v += to_f32(reinterpret_cast<const Out8<O>*>(&old[h])->v[i]);
+        if (a.res) v += old.packed(h * 8 + i);
         y.v[i] = from_f32<O>(v);
       }
       *reinterpret_cast<Out8<O>*>(static_cast<O*>(a.y) + (row + col) * a.ldy + o0 + ch) = y;
     }
   } else if (o0 + lane < a.o) {
-    O* const y = static_cast<O*>(a.y) + o0 + lane;
-    const O* const r = static_cast<const O*>(a.res) + o0 + lane;
-#pragma unroll 4
-    for (int i = 0; i < min(count, 16); ++i) {
+    O* const y = static_cast<O*>(a.y) + row * a.ldy + o0 + lane;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i >= count) break;
       float v = activation<ACT, O>(stage[i * STAGING_LD + lane]);
-      if (a.res) v += to_f32(r[(row + i) * a.ldr]);
-      y[(row + i) * a.ldy] = from_f32<O>(v);
+      if (a.res) v += old.one(i);
+      y[i * a.ldy] = from_f32<O>(v);
     }
   }
 }
@@ -152,15 +173,13 @@ __device__ __forceinline__ void finish(const LinearArgs& a, bool wide, long long
 template <typename O, typename Wait>
 __device__ __forceinline__ void finish_tile(const LinearArgs& a, bool wide, long long row, int rows, int first, int step, int o0, float bias, uint32_t tacc, float* stage,
                                             int lane, Wait wait) {
-  Eight<O> old[2], next[2];
-  const bool ahead = wide && a.res;
-  if (ahead) read_residual<O>(a, row + first, rows - first, o0, lane, next);
+  Old<O> old, next;
+  if (a.res) read_residual<O>(a, wide, row + first, rows - first, o0, lane, next);
   const bool ok = wait();
 #pragma unroll 1
   for (int c = first; c < rows; c += step) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) old[h] = next[h];
-    if (ahead) read_residual<O>(a, row + c + step, rows - c - step, o0, lane, next);
+    old = next;
+    if (a.res) read_residual<O>(a, wide, row + c + step, rows - c - step, o0, lane, next);
     float v[16];
     tmem_ld16(tacc + uint32_t(c), v);
 #pragma unroll
