@@ -1,4 +1,5 @@
-// The dense products of unfolded feed-forward blocks: dispatch, the kernel for every type and size, the weighted return to the tokens.
+// The dense products of unfolded feed-forward blocks: fp32, up to eight rows of bf16, the weighted return to the tokens, and which kernel serves a call
+// (more rows of bf16: linear_tc.cu).
 #include "linear.cuh"
 #include "ptx.cuh"
 

@@ -1,5 +1,5 @@
-// The dense products of the feed-forward blocks that stay unfolded (internal): what the kernels of linear.cu (any type, few
-// rows) and linear_tc.cu (tensor cores) take.
+// The dense products of the feed-forward blocks that stay unfolded (internal): what the kernels of linear.cu (fp32, few rows)
+// and linear_tc.cu (tensor cores) take.
 //   y[r, o] = act(sum_k x[row(r), k] W_e[o, k] + bias_e[o]) + res[r, o]       e = the group of row r
 #pragma once
 #include "common.cuh"

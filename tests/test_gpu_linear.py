@@ -63,7 +63,7 @@ def make(n, k, o, dtype, seed=0, groups=None):
 SIZES = [(1, 8, 1), (1, 256, 1024), (1, 4096, 500), (2, 72, 33), (3, 1032, 129), (4, 4544, 640), (7, 200, 4096), (8, 64, 16), (9, 520, 257),
          (13, 2056, 48), (16, 128, 1000), (17, 1096, 130), (31, 4096, 96), (32, 520, 4544), (33, 776, 100), (64, 2048, 264), (65, 136, 128),
          (100, 264, 127), (128, 512, 512), (129, 1024, 384), (255, 640, 72), (257, 264, 300), (300, 4544, 256), (513, 72, 1025),
-         (777, 328, 272), (1500, 256, 2000), (2049, 1288, 520)]
+         (777, 328, 272), (1500, 256, 2000), (2049, 1288, 520), (20, 8, 40), (200, 16, 300), (1300, 24, 4100)]
 
 
 @gpu
@@ -252,6 +252,21 @@ def test_grouped_with_1024_experts(sizes_at, n):
         for e, size in sorted(sizes_at.items()):
             check(y[at:at + size], *product64(xd[at:at + size], Wd[e], b[e], NONE))
             at += size
+
+
+@gpu
+@pytest.mark.parametrize("n", [5, 40, 2000])
+def test_grouped_rows_of_a_tiny_x(n):
+    """Two rows of x, picked again and again."""
+    x, W, b, _ = make(2, 72, 4100, BF, groups=3)
+    rows = (torch.arange(n, device="cuda") % 3).int()          # 2: no such row
+    xs = torch.cat([x, torch.zeros_like(x[:1])])[rows.long()]
+    sizes = [n // 2, 1, n - n // 2 - 1]
+    y = T.tardis_grouped_linear(x, W, offsets_of(sizes), bias=b, rows=rows)
+    at = 0
+    for e, size in enumerate(sizes):
+        check(y[at:at + size], *product64(xs[at:at + size], W[e], b[e], NONE))
+        at += size
 
 
 @gpu
