@@ -13,7 +13,7 @@ __device__ __forceinline__ void copy16(void* dst, const void* src, bool there) {
 }
 
 // 256 threads compute a tile of ROWS x OUTS, a thread 8 x 8 of them (rows ty + TY i, outputs tx + TX j): what bounds this kernel is reading shared memory, 16 multiply-adds
-// per 16-byte read are what it takes to keep up.  (With 4 x 8 per thread 2048 x 1024 x 2048 took 264 us, with packed multiply-adds too, now 224 = 38
+// per 16-byte read are what it takes to keep up.  (With 4 x 8 per thread 2048 x 1024 x 2048 took 264 us, with packed multiply-adds too, now 220 = 39
 // TFLOP/s; a tile of 32 x 32 with 2 x 2 took 0.6 us for 32 channels.)  Small tiles need fewer threads than that: G groups of them share the channels of a step, and all
 // threads add them up in a fixed order at the end.  Steps of BK channels lie in shared memory as they do in global memory, STAGES - 1 of them on their way (16-byte asynchronous copies).
 template <int ROWS_, int OUTS_, int BK_, int STAGES_> struct CfgF32 {
@@ -72,10 +72,16 @@ __global__ void __launch_bounds__(256, 2) k_linear_f32(const __grid_constant__ L
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const float4*>(sx + C::TY * i * LD + kk);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float4 w = *reinterpret_cast<const float4*>(sw + C::TX * j * LD + kk);
+      for (int j = 0; j < 8; j += 2) {                       // (two outputs at a time: sixteen independent sums; with one 300 x 1024 x 2048 took 62 us, now 54)
+        const float4 w = *reinterpret_cast<const float4*>(sw + C::TX * j * LD + kk), u = *reinterpret_cast<const float4*>(sw + C::TX * (j + 1) * LD + kk);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i][j] = fmaf(x[i].w, w.w, fmaf(x[i].z, w.z, fmaf(x[i].y, w.y, fmaf(x[i].x, w.x, acc[i][j]))));
+        for (int i = 0; i < 8; ++i) { acc[i][j] = fmaf(x[i].x, w.x, acc[i][j]); acc[i][j + 1] = fmaf(x[i].x, u.x, acc[i][j + 1]); }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { acc[i][j] = fmaf(x[i].y, w.y, acc[i][j]); acc[i][j + 1] = fmaf(x[i].y, u.y, acc[i][j + 1]); }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { acc[i][j] = fmaf(x[i].z, w.z, acc[i][j]); acc[i][j + 1] = fmaf(x[i].z, u.z, acc[i][j + 1]); }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { acc[i][j] = fmaf(x[i].w, w.w, acc[i][j]); acc[i][j + 1] = fmaf(x[i].w, u.w, acc[i][j + 1]); }
       }
     }
   }
