@@ -1,5 +1,7 @@
 // The dense products of unfolded feed-forward blocks: fp32, up to eight rows of bf16, the weighted return to the tokens, and which kernel serves a call
 // (more rows of bf16: linear_tc.cu).
+#include <math.h>
+
 #include "linear.cuh"
 #include "ptx.cuh"
 
@@ -206,7 +208,7 @@ static tardis_status_t launch_f32(const LinearArgs& a, cudaStream_t s) {
   return tiles(32, 64) * 10 >= sms * 6 ? launch_f32_tiles<CfgF32<32, 64, 32, 6>>(a, dev, s) : launch_f32_tiles<CfgF32<16, 32, 128, 3>>(a, dev, s);
 }
 
-// ---- up to eight rows of bf16: bound by reading the weights once ----
+// ---- up to eight rows of bf16 (a few times eight of small weights): bound by reading the weights once ----
 // An item is 16 outputs of up to 8 rows of a group.  Weights go straight from global memory into the A fragments of mma.m16n8k16 and the rows of x into its B
 // fragments: a sum over channels may be taken in any order, so lane (g, t) reads 16 bytes, channels 8 t .. 8 t + 7 of a block of 32, of weight rows
 // g and g + 8 and of row g of x, and each pair of words is the fragment of one instruction.  The eight warps of a CTA share the channels in blocks
@@ -221,10 +223,10 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 2) k_linear_few(const __grid_c
   __shared__ float part[2][WARPS][ROWS][17];
   const Groups groups = groups_at(table, a.groups);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int nkb = (a.k + 63) / 64, ot = (a.o + 15) / 16;
+  const int nkb = (a.k + 63) / 64, ot = (a.o + 15) / 16, cuts = (a.n + ROWS - 1) / ROWS;     // (cuts: without groups)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (!a.offsets) {                                        // while the launch before ends: the first steps' weights on their way into L2
-    const int o0 = int((long long)(blockIdx.x) * ot / gridDim.x) * 16;
+    const int o0 = int((long long)(blockIdx.x) * ot * cuts / gridDim.x) / cuts * 16;
     const __nv_bfloat16* const w = static_cast<const __nv_bfloat16*>(a.W) + min(o0 + (lane & 15), a.o - 1) * a.ldw;
     for (int kb = warp + (lane >> 4) * WARPS; kb < min(nkb, 2 * U * WARPS); kb += 2 * WARPS) asm volatile("prefetch.global.L2 [%0];" ::"l"(w + kb * 64));
   }
@@ -233,13 +235,13 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 2) k_linear_few(const __grid_c
     build_groups(a.offsets, a.groups, a.n, ROWS, ot, groups);
     __syncthreads();
   }
-  const int items = a.offsets ? groups.firsts[a.groups] : ot;
+  const int items = a.offsets ? groups.firsts[a.groups] : ot * cuts;
   const int from = int((long long)(blockIdx.x) * items / gridDim.x), to = int((long long)(blockIdx.x + 1) * items / gridDim.x);
   if (from == to) return;
 
   struct Where { int e, o0, first, rows; };
   auto locate = [&](int item) {
-    Where w = {0, item * 16, 0, a.n};
+    Where w = {0, item / cuts * 16, item % cuts * ROWS, min(ROWS, a.n - item % cuts * ROWS)};
     if (a.offsets) {
       const int place = place_of(groups, a.groups, item);
       w.e = groups.order[place];
@@ -333,7 +335,7 @@ static tardis_status_t launch_few(const LinearArgs& a, cudaStream_t s) {
   int dev = 0, sms = 0;
   TARDIS_CUDA_TRY(cudaGetDevice(&dev));
   TARDIS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-  const long long items = (long long)((a.o + 15) / 16) * (a.offsets ? a.n : 1);      // at most (a group's tile has a row)
+  const long long items = (long long)((a.o + 15) / 16) * (a.offsets ? a.n : (a.n + FEW_ROWS - 1) / FEW_ROWS);      // at most (a group's tile has a row)
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(items < 2 * sms ? items : 2 * sms)); cfg.blockDim = dim3(FEW_WARPS * 32); cfg.stream = s;
   cfg.dynamicSmemBytes = a.offsets ? groups_bytes(a.groups) : 0;
@@ -419,8 +421,22 @@ tardis_status_t launch_combine(int tokens, int top_k, const LinearArgs& a, const
 
 tardis_status_t launch_linear(const LinearArgs& a, cudaStream_t s) {
   using namespace linear;
-  if (a.dtype == TARDIS_BF16 && a.n <= FEW_ROWS) return launch_few(a, s);
-  return a.dtype == TARDIS_BF16 ? launch_linear_tc(a, s) : launch_f32(a, s);
+  if (a.dtype == TARDIS_F32) return launch_f32(a, s);
+  if (a.n <= FEW_ROWS) return launch_few(a, s);
+  if (a.n <= 64) {
+    // Rows in several cuts of eight where the weights are small: a launch of the tensor-core kernel takes longer to begin and to end.  A step of two blocks of 64 channels
+    // for each warp takes 0.9 us or the time of the CTAs' 32 KB each, from memory the first time and from L2 for the other cuts.  (Estimate / measured, us: 16 rows of 4096 ->
+    // 4096 13.9 / 12.6, with tcgen05 11.8; 16 of 2048 -> 2048 5.0 / 4.9, 8.1; 24 of 1024 -> 1024 3.6 / 3.7, 7.7; 32 of 1024 -> 4096 8.3 / 9.0, 7.6.)
+    int dev = 0, sms = 0;
+    TARDIS_CUDA_TRY(cudaGetDevice(&dev));
+    TARDIS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    const int groups = a.offsets ? (a.groups < a.n ? a.groups : a.n) : 1, cuts = ((a.n + groups - 1) / groups + FEW_ROWS - 1) / FEW_ROWS;
+    const double items = double((a.o + 15) / 16) * cuts * groups, at_once = 2. * sms, running = items < at_once ? items : at_once;
+    const double step = fmax(0.9, running * 32768 * (1. / cuts / 6.3e6 + (1. - 1. / cuts) / 8e6));
+    const int steps = ((a.k + 63) / 64 + FEW_WARPS * FEW_U - 1) / (FEW_WARPS * FEW_U);
+    if (2.4 + ceil(items / at_once) * (0.2 + steps * step) < estimate_linear_tc(a, sms)) return launch_few(a, s);
+  }
+  return launch_linear_tc(a, s);
 }
 
 }  // namespace tardis

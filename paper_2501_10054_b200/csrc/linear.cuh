@@ -25,6 +25,7 @@ struct LinearArgs {
 
 tardis_status_t launch_linear(const LinearArgs& a, cudaStream_t s);
 tardis_status_t launch_linear_tc(const LinearArgs& a, cudaStream_t s);       // bf16, n > 0
+double estimate_linear_tc(const LinearArgs& a, int sms);                     // us it will take
 // What a gives in fp32 as f [a.n, a.o] (rows of ldf, a multiple of 4), returned to the tokens: a.y[t, o] = a.res[t, o] + sum_j weights[t, j] f[slots[t, j], o]; slots outside
 // the groups add nothing
 tardis_status_t launch_combine(int tokens, int top_k, const LinearArgs& a, const float* f, int ldf, const int* slots, const float* weights,

@@ -556,6 +556,32 @@ static tardis_status_t launch_splits(const LinearArgs& a, int splits, int dev, i
   return launch_rows<1, NT, 1>(a, dev, sms, s);
 }
 
+struct Choice { int kind, splits; double us; };      // kind: 0, 1: 64 or 128 tokens by one CTA; 2: 256 by a pair
+// The variant with the shortest estimate.  A CTA takes some 0.235 us per block of 64 k (less than its MMAs only with 256 tokens), all of them
+// together the time of the weights that they read at once at 6.3 TB/s; clusters of 2, 3 and 4 leave SMs of a GPC unused.  What a launch takes beside
+// that, and a further wave of clusters that exchange parts, is measured too.  (Estimate / measured, us: 128 tokens of 4096 -> 4096, splits of 2 of 64 tokens 16.8 / 15.5, of 4
+// of 128 18.5 / 17.1, whole 64 19.8 / 18.6, 128 20.6 / 20.6; 160 of 4096 -> 16384, 128 35.0 / 37.4, pairs 27.0 / 30.5; 512 of 4096 -> 1024, 4 of 128 16.9 / 15.8.)
+static Choice choose(const LinearArgs& a, int sms) {
+  const int kblocks = (a.k + BK - 1) / BK;
+  const long long groups = a.offsets ? (a.groups < a.n ? a.groups : a.n) : 1, rows = (a.n + groups - 1) / groups;
+  Choice best = {2, 1, 1e30};
+  for (int kind = 0; kind < 3; ++kind)
+    for (int splits = 1; splits <= (kind == 2 ? 1 : 4); ++splits) {
+      if (splits > 1 && kblocks < 4 * splits) continue;
+      const int ctas = kind == 2 ? 2 : 1, most = 64 << kind;
+      const long long cuts = (rows + most - 1) / most, tiles = (a.o + BM * ctas - 1) / (BM * ctas) * cuts * groups;
+      const double width = double((rows + cuts - 1) / cuts), at_once = double(clusters_at_once(sms, splits * ctas));
+      const double waves = ceil(tiles / at_once), running = tiles < at_once ? double(tiles) : at_once;
+      double step = fmax(0.235, running / cuts * (splits * ctas) * (BM * BK * 2) / 6.3e6);
+      if (kind == 2) step = fmax(step, fmax(0.245, 0.275 * width / 256));
+      if (a.rows) step = fmax(step, 0.0035 * width / ctas);                                // (rows picked one by one)
+      double us = waves * ((kblocks + splits - 1) / splits) * step;
+      us += splits == 1 ? 4.0 + 0.012 * width : waves * (3.5 + 0.06 * width) + 2.;
+      if (us < best.us) best = {kind, splits, us};
+    }
+  return best;
+}
+
 // a.work[r] = x[a.rows[r]], a warp per row: 16 bytes per lane
 __global__ void __launch_bounds__(256) k_gather_rows(const __grid_constant__ LinearArgs a) {
   const int r = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, pieces = a.k / 8;
@@ -588,6 +614,8 @@ static tardis_status_t launch_gather_rows(const LinearArgs& a, cudaStream_t s) {
 
 }  // namespace linear
 
+double estimate_linear_tc(const LinearArgs& a, int sms) { return linear::choose(a, sms).us; }
+
 tardis_status_t launch_linear_tc(const LinearArgs& given, cudaStream_t s) {
   using namespace linear;
   LinearArgs a = given;
@@ -595,27 +623,7 @@ tardis_status_t launch_linear_tc(const LinearArgs& given, cudaStream_t s) {
   int dev = 0, sms = 0;
   TARDIS_CUDA_TRY(cudaGetDevice(&dev));
   TARDIS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-  // The variant with the shortest estimate.  A CTA takes some 0.235 us per block of 64 k (less than its MMAs only with 256 tokens), all of them
-  // together the time of the weights that they read at once at 6.3 TB/s; clusters of 2, 3 and 4 leave SMs of a GPC unused.  What a launch takes beside
-  // that, and a further wave of clusters that exchange parts, is measured too.  (Estimate / measured, us: 128 tokens of 4096 -> 4096, splits of 2 of 64 tokens 16.8 / 15.5, of 4
-  // of 128 18.5 / 17.1, whole 64 19.8 / 18.6, 128 20.6 / 20.6; 160 of 4096 -> 16384, 128 35.0 / 37.4, pairs 27.0 / 30.5; 512 of 4096 -> 1024, 4 of 128 16.9 / 15.8.)
-  const int kblocks = (a.k + BK - 1) / BK;
-  const long long groups = a.offsets ? (a.groups < a.n ? a.groups : a.n) : 1, rows = (a.n + groups - 1) / groups;
-  struct Choice { int kind, splits; double us; } best = {2, 1, 1e30};                     // kind: 0, 1: 64 or 128 tokens; 2: pairs, 256
-  for (int kind = 0; kind < 3; ++kind)
-    for (int splits = 1; splits <= (kind == 2 ? 1 : 4); ++splits) {
-      if (splits > 1 && kblocks < 4 * splits) continue;
-      const int ctas = kind == 2 ? 2 : 1, most = 64 << kind;
-      const long long cuts = (rows + most - 1) / most, tiles = (a.o + BM * ctas - 1) / (BM * ctas) * cuts * groups;
-      const double width = double((rows + cuts - 1) / cuts), at_once = double(clusters_at_once(sms, splits * ctas));
-      const double waves = ceil(tiles / at_once), running = tiles < at_once ? double(tiles) : at_once;
-      double step = fmax(0.235, running / cuts * (splits * ctas) * (BM * BK * 2) / 6.3e6);
-      if (kind == 2) step = fmax(step, fmax(0.245, 0.275 * width / 256));
-      if (a.rows) step = fmax(step, 0.0035 * width / ctas);                                // (rows picked one by one)
-      double us = waves * ((kblocks + splits - 1) / splits) * step;
-      us += splits == 1 ? 4.0 + 0.012 * width : waves * (3.5 + 0.06 * width) + 2.;
-      if (us < best.us) best = {kind, splits, us};
-    }
+  const Choice best = choose(a, sms);
   if (best.kind == 2) {
     // Every tile of 256 outputs picks its rows again, at a third of the rate of whole boxes: with scratch and many outputs they are picked once (8192 rows of 4096 -> 16384:
     // 957 us picked tile by tile, 762 picked before; 3800 rows of 16 experts 8192 -> 2048, where the weights of small groups take as long, 170 and 185).
