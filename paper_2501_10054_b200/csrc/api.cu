@@ -381,7 +381,7 @@ tardis_status_t tardis_linear(const tardis_linear_desc_t* d, tardis_stream_t str
   LinearArgs a = {};
   a.n = a.nx = int(d->n); a.k = d->k; a.o = d->o; a.dtype = d->dtype; a.out_dtype = d->out_dtype; a.act = d->act;
   a.x = d->x; a.ldx = d->ldx; a.W = d->W; a.ldw = d->ldw; a.bias = d->bias; a.res = d->residual; a.ldr = d->ldr; a.y = d->y; a.ldy = d->ldy;
-  a.groups = 1;
+  a.groups = 1; a.precise = d->out_dtype == TARDIS_F32;
   if (!linear_args_ok(a, d->n, d->n, d->n)) return TARDIS_ERR_INVALID_ARG;
   if (d->n == 0) return TARDIS_OK;
   if (!linear_pointers_ok(a, d->n, d->n)) return TARDIS_ERR_INVALID_ARG;
@@ -394,7 +394,7 @@ tardis_status_t tardis_grouped_linear(const tardis_grouped_desc_t* d, tardis_str
   a.n = int(d->n_rows); a.nx = int(d->n_x); a.k = d->k; a.o = d->o; a.dtype = d->dtype; a.out_dtype = d->out_dtype; a.act = d->act;
   a.x = d->x; a.ldx = d->ldx; a.W = d->W; a.ldw = d->ldw; a.stride_w = d->stride_w; a.bias = d->bias;
   a.res = d->residual; a.ldr = d->ldr; a.y = d->y; a.ldy = d->ldy;
-  a.groups = d->n_experts; a.offsets = d->offsets; a.rows = d->rows;
+  a.precise = d->out_dtype == TARDIS_F32; a.groups = d->n_experts; a.offsets = d->offsets; a.rows = d->rows;
   const bool back = d->slots || d->weights;
   const long long out_rows = back ? d->n_tokens : d->n_rows;
   if (a.groups <= 0 || !linear_args_ok(a, d->n_rows, d->n_x, out_rows)) return TARDIS_ERR_INVALID_ARG;

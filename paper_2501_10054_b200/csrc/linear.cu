@@ -286,8 +286,9 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 2) k_linear_few(const __grid_c
   };
   const int steps = (nkb + U * WARPS - 1) / (U * WARPS);
   int done = from, step = 0, buf = 0;                      // the computing side
-  float acc[4] = {};
+  float sum[4] = {};                                       // (a step's accumulator starts at zero: the tensor cores cut sums off, and what they lose grows with their number)
   auto compute = [&](const uint4 (&A)[U][4], const uint4 (&B)[U][2]) {
+    float acc[4] = {};
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -296,12 +297,14 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 2) k_linear_few(const __grid_c
         ptx::mma_bf16(acc, v.x, w.x, v.y, w.y, b.x, b.y);
         ptx::mma_bf16(acc, v.z, w.z, v.w, w.w, b.z, b.w);
       }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += acc[i];
     if (++step < steps) return;
     step = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      part[buf][warp][2 * t + (i & 1)][g + 8 * (i >> 1)] = acc[i];
-      acc[i] = 0.f;
+      part[buf][warp][2 * t + (i & 1)][g + 8 * (i >> 1)] = sum[i];
+      sum[i] = 0.f;
     }
     __syncthreads();                                       // (the buffer before is read by threads that have not passed here again)
     if (threadIdx.x < ROWS * 16) {

@@ -11,6 +11,7 @@ constexpr int kMaxExperts = 1024;
 struct LinearArgs {
   int n, k, o;                       // rows of the output, channels, outputs
   int dtype, out_dtype, act;         // act: TARDIS_ACT_NONE or one of tardis_act_t
+  int precise;                       // the call's result is fp32 (out_dtype is, too, where bf16 results are put together from fp32)
   const void* x; long long ldx;      // [nx, k]
   int nx;
   const void* W; long long ldw, stride_w;      // [groups][o, k]

@@ -13,6 +13,10 @@
 // they finish through their shared memory, and the owner of a column adds the parts in the order of their ranks: no atomics, no scratch, the same bits
 // every time.
 //
+// PRECISE (fp32 outputs): the tensor cores cut every sum off to 24 bits, towards zero, so that a long row of products loses 1.5e-8 of the sum per instruction, 1.1e-5 with
+// 11752 channels; the epilogue warps then take the accumulator over after every 512 channels and add it up in registers, rounded to nearest.  (An output of 16 bits does not
+// show it.)
+//
 // Every wait on an mbarrier is bounded: when it runs out the CTA stops issuing, fills what it would have written with NaN and ends after its copies have landed.
 #include <cuda.h>
 #include <math.h>
@@ -27,6 +31,7 @@ using namespace tc;
 
 constexpr int BM = 128, BK = 64, BOX = 32;       // channels of a CTA's tile; k per stage; rows per copy of tokens
 constexpr int NTHREADS = 320, GATHER_WARPS = 4;
+constexpr int PRECISE_BLOCKS = 8;                // k blocks of an accumulator, PRECISE
 
 constexpr int STAGING_LD = 36, STAGING_WARP = 16 * STAGING_LD * 4;    // 16 columns x 32 channels of a warp
 
@@ -169,6 +174,15 @@ __device__ __forceinline__ void finish(const LinearArgs& a, bool wide, long long
     }
   }
 }
+template <typename O>
+__device__ __forceinline__ void finish_as(const LinearArgs& a, bool wide, long long row, int count, int o0, const float* stage, int lane, const Old<O>& old) {
+  switch (a.act) {
+    case TARDIS_ACT_GELU_TANH: finish<TARDIS_ACT_GELU_TANH, O>(a, wide, row, count, o0, stage, lane, old); break;
+    case TARDIS_ACT_GELU_ERF: finish<TARDIS_ACT_GELU_ERF, O>(a, wide, row, count, o0, stage, lane, old); break;
+    case TARDIS_ACT_RELU: finish<TARDIS_ACT_RELU, O>(a, wide, row, count, o0, stage, lane, old); break;
+    default: finish<TARDIS_ACT_NONE, O>(a, wide, row, count, o0, stage, lane, old);
+  }
+}
 // A warp's share of a tile: columns first, first + step, ... in blocks of 16 of the accumulator at `tacc`.  wait() returns whether it has been computed.
 template <typename O, typename Wait>
 __device__ __forceinline__ void finish_tile(const LinearArgs& a, bool wide, long long row, int rows, int first, int step, int o0, float bias, uint32_t tacc, float* stage,
@@ -185,22 +199,17 @@ __device__ __forceinline__ void finish_tile(const LinearArgs& a, bool wide, long
 #pragma unroll
     for (int i = 0; i < 16; ++i) stage[i * STAGING_LD + lane] = ok ? v[i] + bias : CUDART_NAN_F;
     __syncwarp();
-    switch (a.act) {
-      case TARDIS_ACT_GELU_TANH: finish<TARDIS_ACT_GELU_TANH, O>(a, wide, row + c, rows - c, o0, stage, lane, old); break;
-      case TARDIS_ACT_GELU_ERF: finish<TARDIS_ACT_GELU_ERF, O>(a, wide, row + c, rows - c, o0, stage, lane, old); break;
-      case TARDIS_ACT_RELU: finish<TARDIS_ACT_RELU, O>(a, wide, row + c, rows - c, o0, stage, lane, old); break;
-      default: finish<TARDIS_ACT_NONE, O>(a, wide, row + c, rows - c, o0, stage, lane, old);
-    }
+    finish_as<O>(a, wide, row + c, rows - c, o0, stage, lane, old);
     __syncwarp();
   }
 }
 
-template <int CTAS, int NT, int SPLITS, bool GATHER>
+template <int CTAS, int NT, int SPLITS, bool GATHER, bool PRECISE>
 __global__ void __launch_bounds__(NTHREADS + (GATHER ? 32 * GATHER_WARPS : 0), 1)
 k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ Params p) {
   using C = Cfg<CTAS, NT, SPLITS>;
   constexpr bool SPLIT = SPLITS > 1;
-  static_assert(!(SPLIT && CTAS == 2) && C::B_ROWS <= 128, "");
+  static_assert(!(SPLIT && CTAS == 2) && !(PRECISE && CTAS == 2) && C::B_ROWS <= 128, "");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* const exchange = reinterpret_cast<float*>(smem + C::NS * C::STAGE_BYTES);      // [SPLITS][128][PART_LD]
@@ -321,30 +330,33 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     for (int tile = (CTAS == 1 || rank == 0) && nkb > 0 ? first_tile : ntiles; tile < ntiles; tile += step) {
       const Tile t = decode(tile);
       const uint32_t idesc = instr_desc_bf16(BM * CTAS, t.nt);
-      const uint32_t ab = use & 1u;
-      bool ok = mbar_wait_issue(&accum_empty[ab], ((use >> 1) & 1) ^ 1, failed);
-      tc_fence_after();
-      const uint32_t tacc = tmem_base + ab * NT;
-      for (int kb = 0; kb < nkb; ++kb) {
-        ok = mbar_wait_issue(&full[s], parity, failed);
+      const int most = PRECISE ? PRECISE_BLOCKS : nkb;           // k blocks of an accumulator
+      for (int kb0 = 0; kb0 < nkb; kb0 += most) {
+        const uint32_t ab = use & 1u;
+        bool ok = mbar_wait_issue(&accum_empty[ab], ((use >> 1) & 1) ^ 1, failed);
         tc_fence_after();
-        const uint64_t da = adesc + uint32_t(s * (C::STAGE_BYTES >> 4)), db = bdesc + uint32_t(s * (C::STAGE_BYTES >> 4));
-        if (elect_one() && ok) {
+        const uint32_t tacc = tmem_base + ab * NT;
+        for (int kb = kb0; kb < min(nkb, kb0 + most); ++kb) {
+          ok = mbar_wait_issue(&full[s], parity, failed);
+          tc_fence_after();
+          const uint64_t da = adesc + uint32_t(s * (C::STAGE_BYTES >> 4)), db = bdesc + uint32_t(s * (C::STAGE_BYTES >> 4));
+          if (elect_one() && ok) {
 #pragma unroll
-          for (int k = 0; k < BK / 16; ++k) {
-            if (CTAS == 2) umma_f16_pair(tacc, da + k * 2, db + k * 2, idesc, (kb | k) != 0 ? 1u : 0u);
-            else umma_f16(tacc, da + k * 2, db + k * 2, idesc, (kb | k) != 0 ? 1u : 0u);
+            for (int k = 0; k < BK / 16; ++k) {
+              if (CTAS == 2) umma_f16_pair(tacc, da + k * 2, db + k * 2, idesc, (kb != kb0 || k != 0) ? 1u : 0u);
+              else umma_f16(tacc, da + k * 2, db + k * 2, idesc, (kb != kb0 || k != 0) ? 1u : 0u);
+            }
+            if (CTAS == 2) umma_commit_pair(&empty[s]);
+            else umma_commit(&empty[s]);
           }
-          if (CTAS == 2) umma_commit_pair(&empty[s]);
-          else umma_commit(&empty[s]);
+          if (++s == C::NS) { s = 0; parity ^= 1; }
         }
-        if (++s == C::NS) { s = 0; parity ^= 1; }
+        if (elect_one() && ok) {
+          if (CTAS == 2) umma_commit_pair(&accum_full[ab]);
+          else umma_commit(&accum_full[ab]);
+        }
+        ++use;
       }
-      if (elect_one() && ok) {
-        if (CTAS == 2) umma_commit_pair(&accum_full[ab]);
-        else umma_commit(&accum_full[ab]);
-      }
-      ++use;
     }
   } else if (GATHER && warp >= NTHREADS / 32) {
     // ---------------- rows of x by their indices ----------------
@@ -386,12 +398,12 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     // ---------------- epilogue: a warp has TMEM lanes 32 (warp % 4) .. + 31 and every other block of columns ----------------
     const int q = warp & 3, half = (warp - 2) >> 2;
     float* const staging = reinterpret_cast<float*>(smem + C::NS * C::STAGE_BYTES + C::EXCHANGE + (warp - 2) * STAGING_WARP);
-    uint32_t use = 0;
+    uint32_t use = 0, tiles_done = 0;                            // accumulators taken; tiles
     bool ok = true;
     for (int tile = first_tile; tile < ntiles; tile += step) {
       const Tile t = decode(tile);
       const int o = t.o0 + q * 32 + lane;
-      const uint32_t ab = use & 1u;
+      const uint32_t ab = use & 1u;                              // (not PRECISE: the tile's accumulator)
       const float bias = a.bias && o < a.o ? a.bias[(long long)(t.e) * a.o + o] : 0.f;
       auto computed = [&]() {
         if (nkb > 0) ok = ok && mbar_wait_warp(&accum_full[ab], (use >> 1) & 1);
@@ -399,7 +411,49 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         tc_fence_after();
         return ok;
       };
-      if (!SPLIT) {
+      float sum[PRECISE ? NT / 64 : 1][32];                      // PRECISE: columns half * 32 + 64 i + j
+      if (PRECISE) {
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i)
+#pragma unroll
+          for (int j = 0; j < 32; ++j) sum[i][j] = 0.f;
+        for (int kb0 = 0; kb0 < nkb; kb0 += PRECISE_BLOCKS) {
+          const uint32_t a_now = use & 1u;
+          ok = ok && mbar_wait_warp(&accum_full[a_now], (use >> 1) & 1);
+          if (!ok) *failed = 1u;
+          tc_fence_after();
+#pragma unroll
+          for (int i = 0; i < NT / 64; ++i) {
+            if (half * 32 + 64 * i >= t.rows) continue;
+            float v[32];
+            tmem_ld32(tmem_base + a_now * NT + (uint32_t(q * 32) << 16) + uint32_t(half * 32 + 64 * i), v);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum[i][j] += v[j];
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&accum_empty[a_now]);
+          ++use;
+        }
+      }
+      if (PRECISE && !SPLIT) {
+        const int o0 = o - lane;
+        const bool wide = p.wide && o0 + 32 <= a.o;
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i)
+#pragma unroll
+          for (int h = 0; h < 32; h += 16) {
+            const int c = half * 32 + 64 * i + h;
+            if (c >= t.rows) continue;
+            Old<float> old;
+            if (a.res) read_residual<float>(a, wide, t.first + c, t.rows - c, o0, lane, old);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) staging[j * STAGING_LD + lane] = ok ? sum[i][h + j] + bias : CUDART_NAN_F;
+            __syncwarp();
+            finish_as<float>(a, wide, t.first + c, t.rows - c, o0, staging, lane, old);
+            __syncwarp();
+          }
+      } else if (!SPLIT) {
         const int o0 = o - lane;
         const bool wide = p.wide && o0 + 32 <= a.o;
         const uint32_t tacc = tmem_base + ab * NT + (uint32_t(q * 32) << 16);
@@ -423,15 +477,21 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
           }
         };
         read_old(half * 2);
-        computed();
+        if (!PRECISE) computed();
         // of every block of 32 columns, quad i (four columns) belongs to CTA i % SPLITS; the parts of the tile before have been taken by then
-        if (use > 0 && ok) ok = mbar_wait_cluster(parts_empty, (use - 1) & 1);
+        if (tiles_done > 0 && ok) ok = mbar_wait_cluster(parts_empty, (tiles_done - 1) & 1);
         uint32_t to[SPLITS];
 #pragma unroll
         for (int r = 0; r < SPLITS; ++r) to[r] = in_rank(exchange + (rank * BM + q * 32 + lane) * LD, r);
-        for (int c = half * 32; c < t.rows; c += 64) {
+#pragma unroll
+        for (int block = 0; block < NT / 64; ++block) {
+          const int c = half * 32 + 64 * block;
+          if (c >= t.rows) continue;
           float v[32];
-          tmem_ld32(tmem_base + ab * NT + (uint32_t(q * 32) << 16) + uint32_t(c), v);
+          if (PRECISE) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = sum[PRECISE ? block : 0][i];
+          } else tmem_ld32(tmem_base + ab * NT + (uint32_t(q * 32) << 16) + uint32_t(c), v);
           if (!ok || nkb == 0) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = ok ? 0.f : CUDART_NAN_F;
@@ -445,11 +505,11 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          if (nkb > 0) mbar_arrive(&accum_empty[ab]);
+          if (!PRECISE && nkb > 0) mbar_arrive(&accum_empty[ab]);
 #pragma unroll
           for (int r = 0; r < SPLITS; ++r) mbar_arrive_cluster(in_rank(parts_full, r));
         }
-        ok = mbar_wait_cluster(parts_full, use & 1) && ok;
+        ok = mbar_wait_cluster(parts_full, tiles_done & 1) && ok;
         if (!ok) *failed = 1u;
         for (int w0 = half * 2; w0 < QUADS; w0 += 4) {
 #pragma unroll
@@ -479,7 +539,8 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         if (lane == 0)
           for (int r = 0; r < SPLITS; ++r) mbar_arrive_cluster(in_rank(parts_empty, r));
       }
-      ++use;
+      if (!PRECISE) ++use;
+      ++tiles_done;
     }
   }
   tc_fence_before();
@@ -506,7 +567,7 @@ static bool make_weight_map(CUtensorMap* map, const LinearArgs& a) {
   return make_map_3d(map, a.W, a.o, a.groups, a.k, a.ldw, a.groups > 1 ? a.stride_w : a.ldw, BM);
 }
 
-template <int CTAS, int NT, int SPLITS, bool GATHER>
+template <int CTAS, int NT, int SPLITS, bool GATHER, bool PRECISE>
 static tardis_status_t launch(const LinearArgs& a, int dev, int sms, cudaStream_t s) {
   using C = Cfg<CTAS, NT, SPLITS>;
   static_assert(C::FIXED + groups_bytes(kMaxExperts) <= 227 * 1024, "");
@@ -523,7 +584,7 @@ static tardis_status_t launch(const LinearArgs& a, int dev, int sms, cudaStream_
   const int smem = C::FIXED + (a.offsets ? groups_bytes(a.groups) : 0);
   static thread_local int room_on = -1;               // the device on which this thread last gave the kernel its shared memory
   if (dev != room_on) {
-    TARDIS_CUDA_TRY(cudaFuncSetAttribute(k_linear_tc<CTAS, NT, SPLITS, GATHER>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::FIXED + groups_bytes(kMaxExperts)));
+    TARDIS_CUDA_TRY(cudaFuncSetAttribute(k_linear_tc<CTAS, NT, SPLITS, GATHER, PRECISE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::FIXED + groups_bytes(kMaxExperts)));
     room_on = dev;
   }
   long long tiles = (nt + (a.offsets ? (a.groups < a.n ? a.groups : a.n) : 0)) * mt;     // at most
@@ -538,22 +599,22 @@ static tardis_status_t launch(const LinearArgs& a, int dev, int sms, cudaStream_
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = in_cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = in_cluster > 1 ? 2 : 1;
-  TARDIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_linear_tc<CTAS, NT, SPLITS, GATHER>, w, x, p));
+  TARDIS_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_linear_tc<CTAS, NT, SPLITS, GATHER, PRECISE>, w, x, p));
   return TARDIS_OK;
 }
 
-template <int CTAS, int NT, int SPLITS>
+template <int CTAS, int NT, int SPLITS, bool PRECISE>
 static tardis_status_t launch_rows(const LinearArgs& a, int dev, int sms, cudaStream_t s) {
-  return a.rows ? launch<CTAS, NT, SPLITS, true>(a, dev, sms, s) : launch<CTAS, NT, SPLITS, false>(a, dev, sms, s);
+  return a.rows ? launch<CTAS, NT, SPLITS, true, PRECISE>(a, dev, sms, s) : launch<CTAS, NT, SPLITS, false, PRECISE>(a, dev, sms, s);
 }
-template <int NT>
+template <int NT, bool PRECISE>
 static tardis_status_t launch_splits(const LinearArgs& a, int splits, int dev, int sms, cudaStream_t s) {
   switch (splits) {
-    case 2: return launch_rows<1, NT, 2>(a, dev, sms, s);
-    case 3: return launch_rows<1, NT, 3>(a, dev, sms, s);
-    case 4: return launch_rows<1, NT, 4>(a, dev, sms, s);
+    case 2: return launch_rows<1, NT, 2, PRECISE>(a, dev, sms, s);
+    case 3: return launch_rows<1, NT, 3, PRECISE>(a, dev, sms, s);
+    case 4: return launch_rows<1, NT, 4, PRECISE>(a, dev, sms, s);
   }
-  return launch_rows<1, NT, 1>(a, dev, sms, s);
+  return launch_rows<1, NT, 1, PRECISE>(a, dev, sms, s);
 }
 
 struct Choice { int kind, splits; double us; };      // kind: 0, 1: 64 or 128 tokens by one CTA; 2: 256 by a pair
@@ -565,8 +626,8 @@ static Choice choose(const LinearArgs& a, int sms) {
   const int kblocks = (a.k + BK - 1) / BK;
   const long long groups = a.offsets ? (a.groups < a.n ? a.groups : a.n) : 1, rows = (a.n + groups - 1) / groups;
   Choice best = {2, 1, 1e30};
-  for (int kind = 0; kind < 3; ++kind)
-    for (int splits = 1; splits <= (kind == 2 ? 1 : 4); ++splits) {
+  for (int kind = 0; kind < (a.precise ? 2 : 3); ++kind)
+    for (int splits = 1; splits <= (kind == 2 || (a.precise && kind == 1) ? 1 : 4); ++splits) {
       if (splits > 1 && kblocks < 4 * splits) continue;
       const int ctas = kind == 2 ? 2 : 1, most = 64 << kind;
       const long long cuts = (rows + most - 1) / most, tiles = (a.o + BM * ctas - 1) / (BM * ctas) * cuts * groups;
@@ -632,9 +693,10 @@ tardis_status_t launch_linear_tc(const LinearArgs& given, cudaStream_t s) {
       if (st != TARDIS_OK) return st;
       a.x = a.work; a.ldx = a.k; a.nx = a.n; a.rows = nullptr;
     }
-    return launch_rows<2, 256, 1>(a, dev, sms, s);
+    return launch_rows<2, 256, 1, false>(a, dev, sms, s);
   }
-  return best.kind == 1 ? launch_splits<128>(a, best.splits, dev, sms, s) : launch_splits<64>(a, best.splits, dev, sms, s);
+  if (a.precise) return best.kind == 1 ? launch_rows<1, 128, 1, true>(a, dev, sms, s) : launch_splits<64, true>(a, best.splits, dev, sms, s);
+  return best.kind == 1 ? launch_splits<128, false>(a, best.splits, dev, sms, s) : launch_splits<64, false>(a, best.splits, dev, sms, s);
 }
 
 }  // namespace tardis
