@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(NTHREADS + (GATHER ? 32 * GATHER_WARPS : 0), 1
 k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ Params p) {
   using C = Cfg<CTAS, NT, SPLITS>;
   constexpr bool SPLIT = SPLITS > 1;
-  static_assert(!(SPLIT && CTAS == 2) && !(PRECISE && CTAS == 2) && C::B_ROWS <= 128, "");
+  static_assert(!(SPLIT && CTAS == 2) && !(PRECISE && CTAS == 2 && GATHER) && C::B_ROWS <= 128, "");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* const exchange = reinterpret_cast<float*>(smem + C::NS * C::STAGE_BYTES);      // [SPLITS][128][PART_LD]
@@ -425,14 +425,20 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
 #pragma unroll
           for (int i = 0; i < NT / 64; ++i) {
             if (half * 32 + 64 * i >= t.rows) continue;
-            float v[32];
-            tmem_ld32(tmem_base + a_now * NT + (uint32_t(q * 32) << 16) + uint32_t(half * 32 + 64 * i), v);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) sum[i][j] += v[j];
+            for (int h = 0; h < 32; h += 16) {
+              float v[16];
+              tmem_ld16(tmem_base + a_now * NT + (uint32_t(q * 32) << 16) + uint32_t(half * 32 + 64 * i + h), v);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) sum[i][h + j] += v[j];
+            }
           }
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&accum_empty[a_now]);
+          if (lane == 0) {
+            if (CTAS == 2) mbar_arrive_cluster(in_rank_0(&accum_empty[a_now]));
+            else mbar_arrive(&accum_empty[a_now]);
+          }
           ++use;
         }
       }
@@ -626,7 +632,7 @@ static Choice choose(const LinearArgs& a, int sms) {
   const int kblocks = (a.k + BK - 1) / BK;
   const long long groups = a.offsets ? (a.groups < a.n ? a.groups : a.n) : 1, rows = (a.n + groups - 1) / groups;
   Choice best = {2, 1, 1e30};
-  for (int kind = 0; kind < (a.precise ? 2 : 3); ++kind)
+  for (int kind = 0; kind < (a.precise && a.rows ? 2 : 3); ++kind)
     for (int splits = 1; splits <= (kind == 2 || (a.precise && kind == 1) ? 1 : 4); ++splits) {
       if (splits > 1 && kblocks < 4 * splits) continue;
       const int ctas = kind == 2 ? 2 : 1, most = 64 << kind;
@@ -693,7 +699,7 @@ tardis_status_t launch_linear_tc(const LinearArgs& given, cudaStream_t s) {
       if (st != TARDIS_OK) return st;
       a.x = a.work; a.ldx = a.k; a.nx = a.n; a.rows = nullptr;
     }
-    return launch_rows<2, 256, 1, false>(a, dev, sms, s);
+    return a.precise ? launch<2, 256, 1, false, true>(a, dev, sms, s) : launch_rows<2, 256, 1, false>(a, dev, sms, s);      // (with row indices: enough registers for pairs only without PRECISE)
   }
   if (a.precise) return best.kind == 1 ? launch_rows<1, 128, 1, true>(a, dev, sms, s) : launch_splits<64, true>(a, best.splits, dev, sms, s);
   return best.kind == 1 ? launch_splits<128, false>(a, best.splits, dev, sms, s) : launch_splits<64, false>(a, best.splits, dev, sms, s);

@@ -100,8 +100,8 @@ def test_linear_large(n, k, o):
 
 
 @gpu
-@pytest.mark.parametrize("n", [1, 8, 20, 64, 100, 200, 700])
-@pytest.mark.parametrize("k,o", [(11752, 96), (18176, 1000), (1904, 300)])
+@pytest.mark.parametrize("n,k,o", [(n, k, o) for n in (1, 8, 20, 64, 100, 200, 700) for k, o in ((11752, 96), (18176, 1000), (1904, 300))]
+                         + [(1500, 1904, 4100), (2100, 8192, 2048)])
 def test_fp32_outputs_of_many_channels_are_as_near_as_fp32_sums(n, k, o):
     """The tensor cores cut sums off towards zero.  A plain sum of k terms in fp32 is off by some sqrt(k) / 2 roundings of 2^-24 of it, at random; 512 channels of
     cut-off sums lose at most 32 times 2^-24 of their part, on average a third of that: 1e-6 is above both and below what k / 16 cut-offs lose (2.4e-6 of 1904 channels, 1.1e-5 of 11752)."""
