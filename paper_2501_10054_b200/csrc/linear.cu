@@ -422,8 +422,10 @@ tardis_status_t launch_combine(int tokens, int top_k, const LinearArgs& a, const
   return TARDIS_OK;
 }
 
-tardis_status_t launch_linear(const LinearArgs& a, cudaStream_t s) {
+tardis_status_t launch_linear(const LinearArgs& given, cudaStream_t s) {
   using namespace linear;
+  LinearArgs a = given;
+  if (a.k > kMostCutOff) a.precise = 1;
   if (a.dtype == TARDIS_F32) return launch_f32(a, s);
   if (a.n <= FEW_ROWS) return launch_few(a, s);
   if (a.n <= 64) {

@@ -7,11 +7,13 @@
 namespace tardis {
 
 constexpr int kMaxExperts = 1024;
+constexpr int kMostCutOff = 1 << 17;   // channels whose sum may be cut off at every instruction, 1.5e-8 of it each: 1.2e-4, 1/32 of half a step of bf16
 
 struct LinearArgs {
   int n, k, o;                       // rows of the output, channels, outputs
   int dtype, out_dtype, act;         // act: TARDIS_ACT_NONE or one of tardis_act_t
-  int precise;                       // the call's result is fp32 (out_dtype is, too, where bf16 results are put together from fp32)
+  int precise;                       // sums are not left to the tensor cores' cut-off: the call's result is fp32 (out_dtype is, too, where bf16 results are put together from fp32),
+                                     // or there are more than kMostCutOff channels
   const void* x; long long ldx;      // [nx, k]
   int nx;
   const void* W; long long ldw, stride_w;      // [groups][o, k]

@@ -14,8 +14,9 @@
 // every time.
 //
 // PRECISE (fp32 outputs): the tensor cores cut every sum off to 24 bits, towards zero, so that a long row of products loses 1.5e-8 of the sum per instruction, 1.1e-5 with
-// 11752 channels; the epilogue warps then take the accumulator over after every 512 channels and add it up in registers, rounded to nearest.  (An output of 16 bits does not
-// show it.)
+// 11752 channels; the epilogue warps then take the accumulator over after every 512 channels and add it up in registers, rounded to nearest.  Of outputs of 16 bits that is less than 1/32 of
+// their own rounding up to kMostCutOff channels; above, they are computed like this too (in tiles of 64 tokens: in the larger ones both epilogues spill).  That also keeps every wait
+// for an accumulator short, whatever the number of channels is.
 //
 // Every wait on an mbarrier is bounded: when it runs out the CTA stops issuing, fills what it would have written with NaN and ends after its copies have landed.
 #include <cuda.h>
@@ -202,6 +203,26 @@ __device__ __forceinline__ void finish_tile(const LinearArgs& a, bool wide, long
     finish_as<O>(a, wide, row + c, rows - c, o0, stage, lane, old);
     __syncwarp();
   }
+}
+
+// The same of a warp's sums in registers, columns half * 32 + 64 i + j
+template <typename O, int BLOCKS>
+__device__ __forceinline__ void finish_sums(const LinearArgs& a, bool wide, const Tile& t, int half, int o0, bool ok, float bias, const float (&sum)[BLOCKS][32], float* stage,
+                                            int lane) {
+#pragma unroll
+  for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+    for (int h = 0; h < 32; h += 16) {
+      const int c = half * 32 + 64 * i + h;
+      if (c >= t.rows) continue;
+      Old<O> old;
+      if (a.res) read_residual<O>(a, wide, t.first + c, t.rows - c, o0, lane, old);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) stage[j * STAGING_LD + lane] = ok ? sum[i][h + j] + bias : CUDART_NAN_F;
+      __syncwarp();
+      finish_as<O>(a, wide, t.first + c, t.rows - c, o0, stage, lane, old);
+      __syncwarp();
+    }
 }
 
 template <int CTAS, int NT, int SPLITS, bool GATHER, bool PRECISE>
@@ -445,20 +466,8 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       if (PRECISE && !SPLIT) {
         const int o0 = o - lane;
         const bool wide = p.wide && o0 + 32 <= a.o;
-#pragma unroll
-        for (int i = 0; i < NT / 64; ++i)
-#pragma unroll
-          for (int h = 0; h < 32; h += 16) {
-            const int c = half * 32 + 64 * i + h;
-            if (c >= t.rows) continue;
-            Old<float> old;
-            if (a.res) read_residual<float>(a, wide, t.first + c, t.rows - c, o0, lane, old);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) staging[j * STAGING_LD + lane] = ok ? sum[i][h + j] + bias : CUDART_NAN_F;
-            __syncwarp();
-            finish_as<float>(a, wide, t.first + c, t.rows - c, o0, staging, lane, old);
-            __syncwarp();
-          }
+        if (NT == 64 && a.out_dtype == TARDIS_BF16) finish_sums<__nv_bfloat16>(a, wide, t, half, o0, ok, bias, sum, staging, lane);
+        else finish_sums<float>(a, wide, t, half, o0, ok, bias, sum, staging, lane);
       } else if (!SPLIT) {
         const int o0 = o - lane;
         const bool wide = p.wide && o0 + 32 <= a.o;
@@ -631,8 +640,9 @@ struct Choice { int kind, splits; double us; };      // kind: 0, 1: 64 or 128 to
 static Choice choose(const LinearArgs& a, int sms) {
   const int kblocks = (a.k + BK - 1) / BK;
   const long long groups = a.offsets ? (a.groups < a.n ? a.groups : a.n) : 1, rows = (a.n + groups - 1) / groups;
-  Choice best = {2, 1, 1e30};
-  for (int kind = 0; kind < (a.precise && a.rows ? 2 : 3); ++kind)
+  Choice best = {0, 1, 1e30};
+  const int kinds = a.precise && a.out_dtype != TARDIS_F32 ? 1 : a.precise && a.rows ? 2 : 3;
+  for (int kind = 0; kind < kinds; ++kind)
     for (int splits = 1; splits <= (kind == 2 || (a.precise && kind == 1) ? 1 : 4); ++splits) {
       if (splits > 1 && kblocks < 4 * splits) continue;
       const int ctas = kind == 2 ? 2 : 1, most = 64 << kind;
