@@ -161,10 +161,28 @@ __device__ __forceinline__ int place_of(const Groups& t, int groups, int tile) {
   return lo;
 }
 
+// The activations, in one form for all kernels here, so that a token's values do not depend on how many others come with it.  Neither takes a difference of numbers near 1:
+// the negative tails keep their relative accuracy, some units of 2^-24 times z^2 (0.5 z (1 + erf(..)) in fp32 is off by a third at -5).  The erf form: z Phi(z) = max(z, 0) - |z| / 2
+// erfc(|z| / sqrt 2), erfc by the Chebyshev fit of Press et al., Numerical Recipes, section 6.2 (relative error below 1.2e-7 everywhere).  777 tokens of 4544 -> 18176 take 103
+// us without activation, 107 with the tanh form, 112 with this, 120 with erfcf.
+__device__ __forceinline__ float gelu_erf_fit(float z) {
+  const float x = fabsf(z) * 0.7071067811865476f, t = __fdividef(1.f, fmaf(0.5f, x, 1.f));
+  float p = fmaf(0.17087277f, t, -0.82215223f);
+  p = fmaf(p, t, 1.48851587f);
+  p = fmaf(p, t, -1.13520398f);
+  p = fmaf(p, t, 0.27886807f);
+  p = fmaf(p, t, -0.18628806f);
+  p = fmaf(p, t, 0.09678418f);
+  p = fmaf(p, t, 0.37409196f);
+  p = fmaf(p, t, 1.00002368f);
+  p = fmaf(p, t, -1.26551223f);
+  const float half = 0.5f * z;
+  return (half + fabsf(half)) - fminf(fabsf(half), 3.0e38f) * (t * __expf(fmaf(-x, x, p)));
+}
 __device__ __forceinline__ float apply_act(float z, int act) {
   if (act == TARDIS_ACT_NONE) return z;
   if (act == TARDIS_ACT_RELU) return z < 0.f ? 0.f : z;              // (of -inf 0, of NaN NaN)
-  return gelu_f32(z, act);
+  return act == TARDIS_ACT_GELU_TANH ? gelu_tanh_f32(z) : gelu_erf_fit(z);
 }
 __device__ __forceinline__ float load_out(const void* p, long long i, int dtype) {
   return dtype == TARDIS_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : static_cast<const float*>(p)[i];

@@ -91,23 +91,6 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* b, uint32_t parity) 
 // One tile as a role sees it.
 struct Tile { int e, o0, first, rows, nt, turn; };     // group, first output, first row, rows, columns of the MMA, k block to begin with
 
-// The erf form for outputs of 16 bits: z Phi(z) = max(z, 0) - |z| / 2 erfc(|z| / sqrt 2), erfc by formula 7.1.26 of Abramowitz and Stegun (absolute error below
-// 1.5e-7; no difference of numbers near 1 in the negative tail).  777 tokens of 4544 -> 18176 with erff took 128 us.
-__device__ __forceinline__ float gelu_erf_short(float z) {
-  const float x = fabsf(z) * 0.7071067811865476f, t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
-  float poly = fmaf(1.061405429f, t, -1.453152027f);
-  poly = fmaf(poly, t, 1.421413741f);
-  poly = fmaf(poly, t, -0.284496736f);
-  poly = fmaf(poly, t, 0.254829592f);
-  const float half = 0.5f * z;
-  return (half + fabsf(half)) - fminf(fabsf(half), 3.0e38f) * (poly * t * __expf(-x * x));
-}
-template <int ACT, typename O> __device__ __forceinline__ float activation(float z) {
-  if (ACT == TARDIS_ACT_GELU_TANH) return gelu_tanh_f32(z);
-  if (ACT == TARDIS_ACT_GELU_ERF && sizeof(O) == 2) return gelu_erf_short(z);
-  return apply_act(z, ACT);
-}
-
 // The epilogue takes sixteen columns of a warp's 32 channels o0 .. o0 + 31 at a time through shared memory (`stage`, column-major), `count` of them rows of y
 // from `row` on.  Where y and the residual are aligned and all channels are inside, a lane has 8 channels of a token and touches both 16 bytes at a
 // time; else its own channel of all sixteen tokens.  The residual of the next sixteen columns is on its way meanwhile.  (Two bytes per lane throughout: the
@@ -158,7 +141,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, bool wide, long long
       Out8<O> y;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        float v = activation<ACT, O>(z[i]);
+        float v = apply_act(z[i], ACT);
         if (a.res) v += old.packed(h * 8 + i);
         y.v[i] = from_f32<O>(v);
       }
@@ -169,7 +152,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, bool wide, long long
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       if (i >= count) break;
-      float v = activation<ACT, O>(stage[i * STAGING_LD + lane]);
+      float v = apply_act(stage[i * STAGING_LD + lane], ACT);
       if (a.res) v += old.one(i);
       y[i * a.ldy] = from_f32<O>(v);
     }
@@ -543,8 +526,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               if (c + j >= t.rows) break;
-              float y = z[j] + bias;
-              y = a.act == TARDIS_ACT_GELU_TANH ? gelu_tanh_f32(y) : apply_act(y, a.act);
+              float y = apply_act(z[j] + bias, a.act);
               if (a.res) y += old[h * 4 + j];
               store_out(a.y, (t.first + c + j) * a.ldy + o, a.out_dtype, ok ? y : CUDART_NAN_F);
             }

@@ -43,3 +43,52 @@ def test_16_bit_outputs_of_very_many_channels(n, k, o):
     ref, tol = product64(x, W, b, NONE, F32)
     check(T.tardis_linear(x, W, bias=b, out=big[:, 3:3 + o]), ref, tol)
     assert (big[:, :3] == 7).all() and (big[:, 3 + o:] == 7).all()
+
+
+# ---- activations ------------------------------------------------------------------------------------------------
+def act_rows(z, n, dtype):
+    """x [n, 8] and W [len(z), 8] whose product is z in every row, exactly (z of `dtype`)."""
+    x = torch.zeros(n, 8, dtype=dtype, device="cuda")
+    W = torch.zeros(len(z), 8, dtype=dtype, device="cuda")
+    x[:, 0] = 1
+    W[:, 0] = z
+    return x, W
+
+
+@gpu
+@pytest.mark.parametrize("n,dtype,out", [(n, BF, out) for n in (1, 8, 40, 100, 600) for out in (BF, F32)] + [(n, F32, F32) for n in (1, 8, 40, 600)])
+@pytest.mark.parametrize("act", [TANH, ERF])
+def test_tails_of_the_activations(n, dtype, out, act):
+    """Where 1 + tanh or 1 + erf cancels.  Relative to the value: the arguments (z^2 / 2 and about z^2 for the two forms, up to 60 of them here) round three times by 2^-24, the exponential by
+    two units and one more for every 0.86 of its argument (60 / 0.86 + 2 units of 2^-23), a division and products 2^-22: 60 * 3 * 2^-24 + 72 * 2^-23 + 2^-22 < 2e-5; then the output's rounding."""
+    z = -torch.arange(0.0625, 10.0, 0.0625, device="cuda").to(dtype)
+    z = torch.cat([z, -z])
+    x, W = act_rows(z, n, dtype)
+    y = T.tardis_linear(x, W, act=act, out_dtype=out).double()
+    ref = act64(z.double(), act)
+    assert ((y - ref).abs() <= (2e-5 + torch.finfo(out).eps / 2 * 1.001) * ref.abs() + 1e-37).all(), (((y - ref) / ref).abs().max(dim=0).values / 2e-5).max()
+
+
+@gpu
+@pytest.mark.parametrize("act", [NONE, TANH, ERF, RELU])
+@pytest.mark.parametrize("n,dtype", [(1, BF), (8, BF), (40, BF), (100, BF), (600, BF), (1, F32), (8, F32), (40, F32), (600, F32)])
+def test_activations_of_special_values(n, dtype, act):
+    """Very large values of both signs, zeros, infinities and NaN: what the definition gives (the product of -inf and 0 is NaN for the GELU forms, as in the definition)."""
+    z = torch.tensor([0.0, 1e-30, -1e-30, 30.0, -30.0, 1e10, -1e10, 1e19, -1e19, 3e38, -3e38, math.inf, -math.inf, math.nan], device="cuda").to(dtype)
+    x, W = act_rows(z, n, dtype)
+    W[:, 1:] = 0
+    for out in {dtype, F32}:
+        y = T.tardis_linear(x, W, act=act, out_dtype=out).double()
+        ref = act64(z.double(), act).to(out).double().expand(n, -1)
+        assert torch.equal(y.isnan(), ref.isnan()) and torch.equal(y.isinf(), ref.isinf())
+        fine = ref.isfinite()
+        assert ((y - ref)[fine].abs() <= 2.0 ** -20 * ref[fine].abs() + (torch.finfo(out).eps * ref[fine].abs() if out == BF else 0) + 1e-37).all()
+
+
+@gpu
+@pytest.mark.parametrize("n,k,o", [(5, 264, 130), (20, 136, 40), (64, 2048, 264), (100, 1032, 300), (300, 264, 1000), (700, 520, 1032), (1500, 264, 2000)])
+def test_fp32_outputs_of_the_gelu_forms(n, k, o):
+    x, W, b, r = make(n, k, o, BF)
+    for act in (TANH, ERF):
+        for res in (None, r):
+            check(T.tardis_linear(x, W, bias=b, act=act, residual=res, out_dtype=F32), *product64(x, W, b, act, F32), res)
