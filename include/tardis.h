@@ -215,8 +215,8 @@ tardis_status_t tardis_linear(const tardis_linear_desc_t* desc, tardis_stream_t 
  * with row(r) = rows[r], or r without rows.  Without slots, y[r, j] = f[r, j] + residual[r, j]; rows in no group are left as
  * they were.  With slots and weights the rows return to their tokens:
  *     y[t, j] = residual[t, j] + sum_{c < top_k} weights[t, c] f[slots[t, c], j]
- * added in fp32 in the order of c and rounded once; a slot outside offsets[0] .. offsets[n_experts] - 1 (-1, for instance)
- * adds nothing.
+ * added in fp32 in the order of c and rounded once; a slot of no group (outside offsets[0] .. offsets[n_experts] - 1: -1, for
+ * instance) adds nothing.
  *   offsets    device [n_experts + 1], ascending, within 0 .. n_rows (what is not is clamped to the range and to the
  *              offset before: groups never overlap or leave the outputs, whatever the array holds);
  *   rows       device [n_rows] or NULL; an index outside 0 .. n_x - 1 reads as a row of zeros;

@@ -92,3 +92,47 @@ def test_fp32_outputs_of_the_gelu_forms(n, k, o):
     for act in (TANH, ERF):
         for res in (None, r):
             check(T.tardis_linear(x, W, bias=b, act=act, residual=res, out_dtype=F32), *product64(x, W, b, act, F32), res)
+
+
+# ---- groups -----------------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [7, 60, 700])
+def test_return_with_offsets_that_fall(n, dtype):
+    """Groups end where the largest offset so far is: rows that have been computed come back, whatever the last entry says."""
+    x, W, b, _ = make(n, 72, 44, dtype, groups=4)
+    hi = n - 2
+    for off, clamped in (([1, n // 2, hi, hi, 3], [1, n // 2, hi, hi, hi]), ([1, hi, 2, n // 2, 0], [1, hi, hi, hi, hi]), ([-4, n // 2, n + 7, -1, 0], [0, n // 2, n, n, n])):
+        slots = torch.arange(-2, n + 2, dtype=torch.int32, device="cuda")[:, None]
+        w = torch.full((n + 4, 1), 0.5, device="cuda")
+        f = torch.zeros(n + 4, 44, dtype=torch.float64, device="cuda")
+        tol = torch.zeros_like(f)
+        for e in range(4):
+            lo, end = clamped[e], clamped[e + 1]
+            f[2 + lo:2 + end], tol[2 + lo:2 + end] = product64(x[lo:end], W[e], b[e], NONE)
+        work = torch.full((n, 48), float("nan"), device="cuda")
+        y = T.tardis_grouped_linear_combine(x, W, torch.tensor(off, dtype=torch.int32, device="cuda"), slots, w, bias=b, work=work)
+        check(y, 0.5 * f, 0.5 * tol)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,out", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("take", [False, True])
+@pytest.mark.parametrize("tokens,experts,top_k,k,o", [(6, 8, 2, 264, 129), (70, 5, 3, 520, 200), (900, 6, 2, 264, 520), (1300, 4, 2, 136, 1032)])
+def test_return_of_every_form(tokens, experts, top_k, k, o, take, dtype, out):
+    """Both types of result, rows in their order or picked by an index."""
+    _, (_, w, off, _, slots) = routed(tokens, experts, top_k, tokens)
+    n = tokens * top_k
+    x, W, b, r = make(n, k, o, dtype, groups=experts)
+    rows = torch.randint(0, n, (n,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(n), dtype=torch.int32) if take else None
+    xs = x[rows.long()] if take else x
+    f = torch.zeros(n, o, dtype=torch.float64, device="cuda")
+    tol = torch.zeros_like(f)
+    ends = off.tolist()
+    for e in range(experts):
+        own = slice(ends[e], ends[e + 1])
+        f[own], tol[own] = product64(xs[own], W[e], b[e], ERF, out)
+    res = r[:tokens].to(out)
+    y = T.tardis_grouped_linear_combine(x, W, off, slots, w, bias=b, act=ERF, rows=rows, residual=res, out_dtype=out)
+    pick, ww = slots.long(), w.double()[:, :, None]
+    check(y, (f[pick] * ww).sum(1), (tol[pick] * ww + top_k * 2.0 ** -23 * (f[pick] * ww).abs()).sum(1), res)
