@@ -136,3 +136,26 @@ def test_return_of_every_form(tokens, experts, top_k, k, o, take, dtype, out):
     y = T.tardis_grouped_linear_combine(x, W, off, slots, w, bias=b, act=ERF, rows=rows, residual=res, out_dtype=out)
     pick, ww = slots.long(), w.double()[:, :, None]
     check(y, (f[pick] * ww).sum(1), (tol[pick] * ww + top_k * 2.0 ** -23 * (f[pick] * ww).abs()).sum(1), res)
+
+
+@gpu
+@pytest.mark.parametrize("n,experts,o", [(12, 64, 1024), (40, 256, 300), (9, 1024, 512)])
+def test_experts_without_rows_choose_no_other_kernel(n, experts, o):
+    """fp32 rows of a few of many experts are computed as those of the few alone are: the same bits, whatever the number of the others."""
+    k, few = 264, 8
+    x, W, b, _ = make(n, k, o, F32, groups=few)
+    where = torch.linspace(0, experts - 1, few, device="cuda").long()
+    W_all = torch.zeros(experts, o, k, device="cuda")
+    b_all = torch.zeros(experts, o, device="cuda")
+    W_all[where], b_all[where] = W, b
+    sizes = [n // few + (1 if i < n % few else 0) for i in range(few)]
+    all_sizes = [0] * experts
+    for i, e in enumerate(where.tolist()):
+        all_sizes[e] = sizes[i]
+    # (as many groups as rows at most are counted: the few with empty ones up to there)
+    some = min(n, experts)
+    W_some, b_some = torch.zeros(some, o, k, device="cuda"), torch.zeros(some, o, device="cuda")
+    W_some[:few], b_some[:few] = W, b
+    want = T.tardis_grouped_linear(x, W_some, offsets_of(sizes + [0] * (some - few)), bias=b_some)
+    got = T.tardis_grouped_linear(x, W_all, offsets_of(all_sizes), bias=b_all)
+    assert torch.equal(got, want)
