@@ -229,12 +229,13 @@ def _raw_stream(stream, index: int) -> int:
     return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
 
 
-def _empty(x: torch.Tensor, shape, dtype, stream) -> torch.Tensor:
+def _empty(x: torch.Tensor, shape, dtype, stream, zero: bool = False) -> torch.Tensor:
     """Memory for a call on `stream`: taken from that stream's own, which nothing that is still under way on the current one uses."""
+    make = x.new_zeros if zero else x.new_empty
     if stream is None:
-        return x.new_empty(shape, dtype=dtype)
+        return make(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return x.new_empty(shape, dtype=dtype)
+        return make(shape, dtype=dtype)
 
 
 def tardis_linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = TARDIS_ACT_NONE,
@@ -288,8 +289,8 @@ def _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, back, wor
     elif rows is not None and n >= 1024 and o >= 4096 and dtype is torch.bfloat16:       # (where long calls use it)
         work, room = _empty(x, (n, k), dtype, stream), 2 * n * k
         pwork = work.data_ptr()
-    if out is None:
-        out = _empty(x, (n_out, o), out_dtype, stream)
+    if out is None:                                          # (rows in no group are left as they were: zero)
+        out = _empty(x, (n_out, o), out_dtype, stream, zero=back is None)
     px, ldx = _matrix(x, "x", dtype, nx, k, index)
     stride_w, ldw, unit = W.stride()
     if W.dtype is not dtype or W.get_device() != index or unit != 1:
@@ -310,7 +311,8 @@ def tardis_grouped_linear(x: torch.Tensor, W: torch.Tensor, offsets: torch.Tenso
                           out: Optional[torch.Tensor] = None, out_dtype=None, stream=None):
     """The product of tardis_linear with each group's own weights (see tardis_grouped_linear in tardis.h): W [experts, o, k], bias
     [experts, o], offsets int32 [experts + 1] on the device; y[r] = act(W_e x[rows[r]] + bias_e) + residual[r] for
-    offsets[e] <= r < offsets[e + 1].  Rows of `out` in no group are left as they were."""
+    offsets[e] <= r < offsets[e + 1].  Rows of `out` in no group are left as they were; of a result that is made here they are zero (which
+    costs a pass over it: programs that read rows in groups only, as the return to the tokens does, bring `out`)."""
     return _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, None, None, stream, "tardis_grouped_linear")
 
 

@@ -159,3 +159,17 @@ def test_experts_without_rows_choose_no_other_kernel(n, experts, o):
     want = T.tardis_grouped_linear(x, W_some, offsets_of(sizes + [0] * (some - few)), bias=b_some)
     got = T.tardis_grouped_linear(x, W_all, offsets_of(all_sizes), bias=b_all)
     assert torch.equal(got, want)
+
+
+# ---- the binding ------------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rows_in_no_group_of_a_fresh_output_are_zero(dtype):
+    n, k, o = 300, 64, 48
+    x, W, b, r = make(n, k, o, dtype, groups=2)
+    for _ in range(3):
+        stale = torch.full((n, o), float("nan"), dtype=dtype, device="cuda")
+        del stale                                              # (the memory that a fresh output of this size gets)
+        y = T.tardis_grouped_linear(x, W, torch.tensor([4, 100, 250], dtype=torch.int32, device="cuda"), bias=b)
+        assert (y[:4] == 0).all() and (y[250:] == 0).all() and y.isfinite().all()
+        check(y[4:100], *product64(x[4:100], W[0], b[0], NONE))
