@@ -8,6 +8,7 @@ no CPU fallback: importing works anywhere, but any call needs libtardis.so and a
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 import struct
 from typing import Optional
@@ -199,6 +200,19 @@ def tardis_gemm_bf16(A: torch.Tensor, B: torch.Tensor, C: torch.Tensor, stream=N
 # a few microseconds on the device should not take longer to describe.
 _PACK_LINEAR = struct.Struct("@qiiiiiPqPqPPqPq").pack
 _PACK_GROUPED = struct.Struct("@qiiiiiiPqqPqqPPPPqPqqiPPPN").pack
+_ACTS = (TARDIS_ACT_NONE, TARDIS_ACT_GELU_TANH, TARDIS_ACT_GELU_ERF, TARDIS_ACT_RELU)
+
+
+def _whole(v, name: str) -> int:
+    try:
+        return operator.index(v)
+    except TypeError:
+        raise TardisError(1, "%s must be a whole number" % name) from None
+
+
+def _check_act(act) -> None:
+    if _whole(act, "act") not in _ACTS:
+        raise TardisError(1, "act must be TARDIS_ACT_NONE, TARDIS_ACT_GELU_TANH, TARDIS_ACT_GELU_ERF or TARDIS_ACT_RELU")
 
 
 def _current(x: torch.Tensor) -> int:
@@ -211,7 +225,10 @@ def _current(x: torch.Tensor) -> int:
 
 def _matrix(t: torch.Tensor, name: str, dtype, rows: int, cols: int, index: int):
     """(data pointer, leading dimension) of a matrix with unit inner stride."""
-    shape, (ld, unit) = t.shape, t.stride()
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2:
+        raise TardisError(1, "%s must be a matrix" % name)
+    ld, unit = strides
     if t.dtype is not dtype or shape[0] != rows or shape[1] != cols or t.get_device() != index or (unit != 1 and cols > 1):
         raise TardisError(1, "%s must be a %s matrix of %d x %d on the same device with unit inner stride" % (name, dtype, rows, cols))
     return t.data_ptr(), ld if rows > 1 else cols
@@ -245,6 +262,7 @@ def tardis_linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor]
     when given; it may be the residual)."""
     if x.dim() != 2 or W.dim() != 2 or W.shape[1] != x.shape[1]:
         raise TardisError(1, "x must be [n, k] and W [o, k]")
+    _check_act(act)
     index, dtype = _current(x), x.dtype
     (n, k), o = x.shape, W.shape[0]
     if out_dtype is None:
@@ -266,6 +284,7 @@ def tardis_linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor]
 def _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, back, work, stream, what):
     if x.dim() != 2 or W.dim() != 3 or W.shape[2] != x.shape[1]:
         raise TardisError(1, "x must be [n, k] and W [experts, o, k]")
+    _check_act(act)
     index, dtype, i32 = _current(x), x.dtype, torch.int32
     (nx, k), (experts, o, _) = x.shape, W.shape
     n = nx if rows is None else rows.numel()
@@ -335,6 +354,7 @@ def tardis_route(logits: torch.Tensor, top_k: int, normalise: bool = True, strea
     index = _current(logits)
     n, e = logits.shape
     pl, ldl = _matrix(logits, "logits", torch.float32, n, e, index)
+    top_k = _whole(top_k, "top_k")
     if not 1 <= top_k <= e:
         raise TardisError(1, "top_k must be between 1 and the number of experts")
     i32 = torch.int32

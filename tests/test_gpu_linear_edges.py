@@ -173,3 +173,22 @@ def test_rows_in_no_group_of_a_fresh_output_are_zero(dtype):
         y = T.tardis_grouped_linear(x, W, torch.tensor([4, 100, 250], dtype=torch.int32, device="cuda"), bias=b)
         assert (y[:4] == 0).all() and (y[250:] == 0).all() and y.isfinite().all()
         check(y[4:100], *product64(x[4:100], W[0], b[0], NONE))
+
+
+@gpu
+def test_binding_refuses_what_is_no_matrix_or_number():
+    x, W, b, r = make(4, 64, 24, BF)
+    off = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    slots, w = torch.zeros(4, 1, dtype=torch.int32, device="cuda"), torch.zeros(4, 1, device="cuda")
+    flat = torch.zeros(96, dtype=BF, device="cuda")
+    for call in (lambda: T.tardis_linear(x, W, out=flat), lambda: T.tardis_linear(x, W, residual=flat), lambda: T.tardis_linear(x, W, out=flat.view(1, 4, 24)),
+                 lambda: T.tardis_linear(x, W, act=None), lambda: T.tardis_linear(x, W, act=1.5), lambda: T.tardis_linear(x, W, act=1 << 40),
+                 lambda: T.tardis_grouped_linear(x, W[None], off, out=flat), lambda: T.tardis_grouped_linear(x, W[None], off, residual=flat),
+                 lambda: T.tardis_grouped_linear(x, W[None], off, act="relu"),
+                 lambda: T.tardis_grouped_linear_combine(x, W[None], off, slots, w, residual=flat),
+                 lambda: T.tardis_grouped_linear_combine(x, W[None], off, slots, w, work=torch.zeros(8, device="cuda")),
+                 lambda: T.tardis_route(torch.zeros(4, 8, device="cuda"), 1.5), lambda: T.tardis_route(torch.zeros(4, 8, device="cuda"), None)):
+        with pytest.raises(T.TardisError):
+            call()
+    assert torch.equal(T.tardis_linear(x, W, act=np.int64(RELU)), T.tardis_linear(x, W, act=RELU))          # (whole numbers of any type)
+    assert T.tardis_route(torch.zeros(4, 8, device="cuda"), np.int64(3))[0].shape == (4, 3)
