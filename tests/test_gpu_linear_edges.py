@@ -176,6 +176,22 @@ def test_rows_in_no_group_of_a_fresh_output_are_zero(dtype):
 
 
 @gpu
+def test_no_scratch_for_calls_that_use_none():
+    """fp32 outputs pick their rows tile by tile: n k bf16 of scratch would never be touched."""
+    n, k, o = 2048, 4096, 4096
+    x, W, _, _ = make(n, k, o, BF, groups=1)
+    rows, off = torch.arange(n, dtype=torch.int32, device="cuda"), torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    y = torch.empty(n, o, device="cuda")
+    T.tardis_grouped_linear(x, W, off, rows=rows, out=y)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    T.tardis_grouped_linear(x, W, off, rows=rows, out=y)
+    assert torch.cuda.max_memory_allocated() == before
+    check(y, *product64(x, W[0], None, NONE, F32))
+
+
+@gpu
 def test_binding_refuses_what_is_no_matrix_or_number():
     x, W, b, r = make(4, 64, 24, BF)
     off = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
