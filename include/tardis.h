@@ -191,7 +191,7 @@ tardis_status_t tardis_gemm_bf16(int32_t M, int32_t N, int32_t K, const void* A,
  *   act        tardis_act_t or TARDIS_ACT_NONE;
  *   x, W       device, row-major, 16-byte aligned; k, ldx and ldw multiples of 8;
  *   bias, residual   device or NULL; y: any ldy >= o, any element-aligned start.
- * y may be residual (in place, with ldr = ldy) and overlaps none of the other inputs.  n = 0 does nothing.  Asynchronous
+ * y may be residual (in place, with ldr = ldy) and overlaps none of the other inputs (INVALID_ARG).  n = 0 does nothing.  Asynchronous
  * on `stream`; allocates nothing; nothing is kept; the same bits from run to run.  (Should a wait inside the tensor-core
  * kernel run out, which no valid call makes happen, the tile concerned is filled with NaN.)
  * Errors: INVALID_ARG, UNSUPPORTED (driver without tensor-map support; more than 8 million outputs of fp32), CUDA. */
@@ -224,7 +224,8 @@ tardis_status_t tardis_linear(const tardis_linear_desc_t* desc, tardis_stream_t 
  *   work       device scratch, 16-byte aligned, caller-owned (calls that overlap in time need one each).  With slots at
  *              least 4 n_rows o8 bytes, o8 = o rounded up to a multiple of 8.  Else it may be NULL; with rows, bf16 operands and outputs, at
  *              least 4096 outputs and 2 n_rows k bytes of scratch, long calls gather the rows there once instead of picking them again for
- *              every tile of outputs (calls with fp32 outputs never do: their tiles are not those of pairs of CTAs).
+ *              every tile of outputs (calls with fp32 outputs never do: their tiles are not those of pairs of CTAs).  It
+ *              overlaps no other array.
  * Other arguments, alignment, result and errors as for tardis_linear; n_experts <= 1024 (UNSUPPORTED beyond). */
 typedef struct {
   int64_t n_rows;             /* rows of f: (token, choice) pairs; below 2^31 - 4096 */

@@ -355,6 +355,30 @@ static bool linear_args_ok(const LinearArgs& a, long long n, long long nx, long 
   if (a.k % 8 || a.ldx % 8 || a.ldw % 8 || a.ldx < a.k || a.ldw < a.k || a.ldy < a.o || (a.res && a.ldr < a.o)) return false;
   return a.ldx <= kMostLd && a.ldw <= kMostLd && a.ldy <= kMostLd && (!a.res || a.ldr <= kMostLd) && a.stride_w <= kMostLd;
 }
+// whether `bytes` from p on share memory with y (they may lie between two of its rows)
+static bool linear_output_meets(const LinearArgs& a, long long out_rows, const void* p, long long bytes) {
+  const uintptr_t p0 = reinterpret_cast<uintptr_t>(p), y0 = reinterpret_cast<uintptr_t>(a.y);
+  const long long out = a.out_dtype == TARDIS_BF16 ? 2 : 4, ld = a.ldy * out, width = a.o * out;
+  if (!p || bytes <= 0 || p0 >= y0 + (out_rows - 1) * ld + width || y0 >= p0 + bytes) return false;
+  const long long apart = p0 < y0 ? 0 : (long long)(p0 - y0) % ld;
+  return apart < width || apart + bytes > ld;
+}
+static long long linear_weight_bytes(const LinearArgs& a) {
+  return ((a.groups - 1) * a.stride_w + (a.o - 1) * a.ldw + a.k) * (a.dtype == TARDIS_BF16 ? 2 : 4);
+}
+// Scratch is written while everything else is still read, and read while y is written: it may share memory with none of them.
+static bool grouped_scratch_apart(const LinearArgs& a, const tardis_grouped_desc_t& d, long long out_rows, size_t room) {
+  const long long in = a.dtype == TARDIS_BF16 ? 2 : 4, out = a.out_dtype == TARDIS_BF16 ? 2 : 4, choices = d.slots ? out_rows * d.top_k * 4ll : 0;
+  const struct { const void* p; long long bytes; } others[] = {
+      {a.y, ((out_rows - 1) * a.ldy + a.o) * out}, {a.res, ((out_rows - 1) * a.ldr + a.o) * out}, {a.x, d.n_x > 0 ? ((d.n_x - 1) * a.ldx + a.k) * in : 0},
+      {a.W, linear_weight_bytes(a)}, {a.bias, 4ll * a.groups * a.o}, {a.offsets, (a.groups + 1) * 4ll}, {a.rows, a.n * 4ll}, {d.slots, choices}, {d.weights, choices}};
+  const uintptr_t w0 = reinterpret_cast<uintptr_t>(d.work);
+  for (const auto& o : others) {
+    const uintptr_t p0 = reinterpret_cast<uintptr_t>(o.p);
+    if (o.p && o.bytes > 0 && p0 < w0 + room && w0 < p0 + o.bytes) return false;
+  }
+  return true;
+}
 static bool linear_pointers_ok(const LinearArgs& a, long long nx, long long out_rows) {
   if (!a.y || (a.n > 0 && (!a.x || !a.W)) || !aligned16(a.x) || !aligned16(a.W)) return false;
   const long long in = a.dtype == TARDIS_BF16 ? 2 : 4, out = a.out_dtype == TARDIS_BF16 ? 2 : 4;
@@ -372,7 +396,8 @@ static bool linear_pointers_ok(const LinearArgs& a, long long nx, long long out_
     return apart < y_width || apart + width > ld;
   };
   if (meets(a.x, nx, a.ldx * in, a.k * in) || meets(a.bias, a.groups, a.o * 4ll, a.o * 4ll)) return false;
-  if (meets(a.W, 1, 0, ((a.groups - 1) * a.stride_w + (a.o - 1) * a.ldw + a.k) * in)) return false;
+  if (linear_output_meets(a, out_rows, a.W, linear_weight_bytes(a)) || linear_output_meets(a, out_rows, a.offsets, (a.groups + 1) * 4ll) || linear_output_meets(a, out_rows, a.rows, a.n * 4ll))
+    return false;
   return !(meets(a.res, out_rows, a.ldr * out, a.o * out) && !(a.res == a.y && a.ldr == a.ldy));
 }
 
@@ -406,14 +431,17 @@ tardis_status_t tardis_grouped_linear(const tardis_grouped_desc_t* d, tardis_str
   if (!linear_pointers_ok(a, d->n_x, out_rows)) return TARDIS_ERR_INVALID_ARG;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (!back) {
-    if (d->work && !aligned16(d->work)) return TARDIS_ERR_INVALID_ARG;
-    if (d->work_bytes >= size_t(a.n) * size_t(a.k) * 2) a.work = d->work;
+    const size_t room = size_t(a.n) * size_t(a.k) * 2;
+    if (d->work && (!aligned16(d->work) || (d->work_bytes >= room && !grouped_scratch_apart(a, *d, out_rows, room)))) return TARDIS_ERR_INVALID_ARG;
+    if (d->work_bytes >= room) a.work = d->work;
     return launch_linear(a, s);
   }
   if ((reinterpret_cast<uintptr_t>(d->slots) | reinterpret_cast<uintptr_t>(d->weights)) & 3u) return TARDIS_ERR_INVALID_ARG;
+  const long long choices = out_rows * d->top_k * 4ll;
+  if (linear_output_meets(a, out_rows, d->slots, choices) || linear_output_meets(a, out_rows, d->weights, choices)) return TARDIS_ERR_INVALID_ARG;
   const int ldf = (a.o + 7) & ~7;                            // (so that rows are aligned whatever o is)
   const size_t room = size_t(a.n) * size_t(ldf) * 4;
-  if (room > 0 && (!d->work || !aligned16(d->work) || d->work_bytes < room)) return TARDIS_ERR_INVALID_ARG;
+  if (room > 0 && (!d->work || !aligned16(d->work) || d->work_bytes < room || !grouped_scratch_apart(a, *d, out_rows, room))) return TARDIS_ERR_INVALID_ARG;
   LinearArgs f = a;
   f.res = nullptr; f.y = d->work; f.ldy = ldf; f.out_dtype = TARDIS_F32;
   if (f.n > 0) {

@@ -208,3 +208,45 @@ def test_binding_refuses_what_is_no_matrix_or_number():
             call()
     assert torch.equal(T.tardis_linear(x, W, act=np.int64(RELU)), T.tardis_linear(x, W, act=RELU))          # (whole numbers of any type)
     assert T.tardis_route(torch.zeros(4, 8, device="cuda"), np.int64(3))[0].shape == (4, 3)
+
+
+# ---- refusals (no device needed) --------------------------------------------------------------------------------
+@pytest.mark.parametrize("change", [
+    dict(work=(1 << 22) + 16), dict(work=1 << 20), dict(work=(1 << 21) + 3 * 24 * 64 * 2 - 16), dict(work=(1 << 23) - 16), dict(work=(1 << 24) - 560), dict(work=1 << 25),
+    dict(residual=(1 << 26) + 64, ldr=24), dict(bias=(1 << 26) + 64), dict(rows=(1 << 26) + 572), dict(slots=(1 << 22) + 4), dict(weights=(1 << 22) + 3 * 48 - 4),
+    dict(offsets=(1 << 22) + 8), dict(rows=(1 << 22) - 20)])
+def test_scratch_and_indices_that_share_memory_are_refused(change):
+    import ctypes
+
+    from paper_2501_10054_b200 import build
+    from tests.test_gpu_linear import BACK, GROUPED
+    build.build()
+    assert T.load_library().tardis_grouped_linear(ctypes.byref(T.GroupedDesc(**{**GROUPED, **BACK, **change})), None) == 1
+
+
+@pytest.mark.parametrize("change", [dict(offsets=(1 << 22) + 8), dict(rows=(1 << 22) - 20), dict(rows=(1 << 22) + 284),
+                                    dict(rows=1 << 24, work=(1 << 24) - 752, work_bytes=768), dict(rows=1 << 24, work=1 << 20, work_bytes=768),
+                                    dict(rows=1 << 24, work=(1 << 22) + 272, work_bytes=768)])
+def test_indices_and_gathered_rows_that_share_memory_are_refused(change):
+    import ctypes
+
+    from paper_2501_10054_b200 import build
+    from tests.test_gpu_linear import GROUPED
+    build.build()
+    assert T.load_library().tardis_grouped_linear(ctypes.byref(T.GroupedDesc(**{**GROUPED, **change})), None) == 1
+
+
+@gpu
+def test_matrices_side_by_side_in_one_buffer_are_no_overlap():
+    """Columns of one buffer that do not meet: x, residual and y, and indices between two rows of y."""
+    n, k, o = 12, 64, 24
+    buf = torch.randn(n, 256, device="cuda").to(BF)
+    x, r, y = buf[:, :k], buf[:, k:k + o], buf[:, 96:96 + o]
+    off, rows = buf[2, 128:132].view(torch.int32), buf[3, 128:152].view(torch.int32)
+    off.copy_(torch.tensor([0, n], dtype=torch.int32))
+    rows.copy_(torch.arange(n - 1, -1, -1, dtype=torch.int32))
+    W = (torch.randn(1, o, k, device="cuda") * 0.1).to(BF)
+    ref, tol = product64(x.flip(0), W[0], None, NONE)
+    T.tardis_grouped_linear(x, W, off, rows=rows, residual=r, out=y)
+    check(y, ref, tol, r)
+    assert torch.equal(rows, torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda"))
