@@ -218,6 +218,13 @@ static tardis_status_t launch_f32(const LinearArgs& a, cudaStream_t s) {
 // multiplied, summed up and stored.
 constexpr int FEW_ROWS = 8, FEW_WARPS = 8, FEW_U = 2;      // U: blocks of 64 channels of a warp and step
 
+// Weights pass L1 by.  Not the read-only path: this kernel begins while the launch before, which may write what is read here, is still running.
+__device__ __forceinline__ uint4 load_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+
 __global__ void __launch_bounds__(FEW_WARPS * 32, 2) k_linear_few(const __grid_constant__ LinearArgs a) {
   constexpr int ROWS = FEW_ROWS, WARPS = FEW_WARPS, U = FEW_U;
   extern __shared__ int table[];                           // (grouped only)
@@ -275,8 +282,8 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 2) k_linear_few(const __grid_c
       for (int h = 0; h < 2; ++h) {
         const int k = (kb + u * WARPS) * 64 + h * 32;
         const bool in = k + t * 8 < a.k;
-        A[u][h] = in ? ptx::ldg_stream(w0 + k) : make_uint4(0u, 0u, 0u, 0u);
-        A[u][2 + h] = in ? ptx::ldg_stream(w1 + k) : make_uint4(0u, 0u, 0u, 0u);
+        A[u][h] = in ? load_once(w0 + k) : make_uint4(0u, 0u, 0u, 0u);
+        A[u][2 + h] = in ? load_once(w1 + k) : make_uint4(0u, 0u, 0u, 0u);
         B[u][h] = in && there ? *reinterpret_cast<const uint4*>(x + k) : make_uint4(0u, 0u, 0u, 0u);
       }
     kb += U * WARPS;
@@ -355,8 +362,8 @@ static tardis_status_t launch_few(const LinearArgs& a, cudaStream_t s) {
 // A thread adds up four outputs of a token, its choices in their order (four loads of f under way at a time).  wide: y and the residual are touched four at a time too.
 // (Eight CTAs per SM: with six, what more registers than 32 leave, 4096 tokens of 4096 outputs took 194 us with their product, now 177.)
 template <typename O>
-__global__ void __launch_bounds__(256, 8) k_combine(const __grid_constant__ LinearArgs a, int top_k, const float* __restrict__ f, int ldf,
-                                                 const int* __restrict__ slots, const float* __restrict__ weights, int wide) {
+__global__ void __launch_bounds__(256, 8) k_combine(const __grid_constant__ LinearArgs a, int top_k, const float* f, int ldf, const int* slots,
+                                                                  const float* weights, int wide) {
   struct alignas(4 * sizeof(O)) Out { O v[4]; };
   const long long t = blockIdx.x;
   const int c = (blockIdx.y * 256 + threadIdx.x) * 4;

@@ -161,6 +161,43 @@ def test_experts_without_rows_choose_no_other_kernel(n, experts, o):
     assert torch.equal(got, want)
 
 
+@gpu
+@pytest.mark.parametrize("n", [1, 4, 8, 20, 200])
+def test_weights_and_rows_written_by_the_launch_before(n):
+    """A launch begins while the one before is still running: weights, rows and slots that that one writes, at the same place every time, are read as written."""
+    k, o, rounds = 1024, 512, 12
+    x, _, b, _ = make(n, k, o, BF)
+    low = [make(o, 64, k, BF, seed=i)[0] for i in range(rounds)]
+    _, up, _, _ = make(1, 64, k, BF, seed=77)                  # W = low up^T: [o, k]
+    logits = [torch.randn(n, 4, device="cuda", generator=torch.Generator(device="cuda").manual_seed(i)) for i in range(rounds)]
+    W, y, back = torch.zeros(4, o, k, dtype=BF, device="cuda"), torch.zeros(2 * n, o, dtype=BF, device="cuda"), torch.zeros(n, k, dtype=BF, device="cuda")
+    _, W2, _, _ = make(1, o, k, BF, seed=5, groups=4)
+    work = torch.zeros(2 * n, k, device="cuda")
+
+    def step(i):
+        _, w, off, rows, slots = T.tardis_route(logits[i], 2)
+        for e in range(4):
+            T.tardis_linear(low[i].roll(e, 0), up, out=W[e])
+        T.tardis_linear(x, W[3], out=y[:n])
+        first = y[:n].clone()
+        T.tardis_grouped_linear(x, W, off, rows=rows, act=RELU, out=y)
+        T.tardis_grouped_linear_combine(y, W2, off, slots, w, out=back, work=work)
+        return first, y.clone(), back.clone()
+
+    apart = []
+    for i in range(rounds):
+        got = step(i)
+        torch.cuda.synchronize()
+        apart.append(got)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        together = [step(i) for i in range(rounds)]
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for i in range(rounds) for p, q in zip(apart[i], together[i]))
+
+
 # ---- the binding ------------------------------------------------------------------------------------------------
 @gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
