@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2501_10054_b200 as T
-from tests.test_gpu_linear import BF, ERF, F32, NONE, RELU, TANH, act64, check, gpu, make, offsets_of, product64, routed
+from tests.test_gpu_linear import BF, ERF, F32, NONE, RELU, TANH, act64, check, check_route, gpu, make, offsets_of, product64, routed
 
 
 # ---- very many channels -----------------------------------------------------------------------------------------
@@ -94,6 +94,16 @@ def test_fp32_outputs_of_the_gelu_forms(n, k, o):
             check(T.tardis_linear(x, W, bias=b, act=act, residual=res, out_dtype=F32), *product64(x, W, b, act, F32), res)
 
 
+# ---- second products of hundreds of rows ------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("n,k,o", [(100, 16384, 2048), (160, 16384, 4096), (256, 16384, 4096), (384, 16384, 4096), (512, 18176, 4544), (500, 11752, 1000)])
+def test_second_products_of_hundreds_of_rows(n, k, o):
+    x, W, b, r = make(n, k, o, BF)
+    for out in (BF, F32):
+        res = r.to(out)
+        check(T.tardis_linear(x, W, bias=b, residual=res, out_dtype=out), *product64(x, W, b, NONE, out), res)
+
+
 # ---- groups -----------------------------------------------------------------------------------------------------
 @gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -162,6 +172,48 @@ def test_experts_without_rows_choose_no_other_kernel(n, experts, o):
 
 
 @gpu
+def test_group_sizes_change_between_replays():
+    """One captured call; the sizes of the groups, the rows and the slots change on the device: even, all in one group, skewed, none."""
+    tokens, experts, top_k, k, o = 700, 6, 2, 136, 4104
+    n = tokens * top_k
+    x, W, b, _ = make(tokens, k, o, BF, groups=experts)
+    _, W2, b2, _ = make(1, o, 72, BF, groups=experts)
+    off, rows = torch.zeros(experts + 1, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    slots, w = torch.zeros(tokens, top_k, dtype=torch.int32, device="cuda"), torch.zeros(tokens, top_k, device="cuda")
+    y = torch.zeros(n, o, dtype=BF, device="cuda")
+
+    def block():
+        T.tardis_grouped_linear(x, W, off, bias=b, act=RELU, rows=rows, out=y)
+        return T.tardis_grouped_linear_combine(y, W2, off, slots, w, bias=b2)
+
+    block()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        back = block()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for tilt in (0.0, 20.0, 3.0, -math.inf):
+        logits = torch.randn(tokens, experts, generator=g, device="cuda")
+        logits = torch.full_like(logits, tilt) if tilt < 0 else logits + tilt * torch.arange(experts, device="cuda") / experts
+        _, w_new, off_new, rows_new, slots_new = T.tardis_route(logits, top_k)
+        for dst, src in ((w, w_new), (off, off_new), (rows, rows_new), (slots, slots_new)):
+            dst.copy_(src)
+        y.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        ends = off.tolist()
+        f, tol = torch.zeros(n, 72, dtype=torch.float64, device="cuda"), torch.zeros(n, 72, dtype=torch.float64, device="cuda")
+        for e in range(experts):
+            own = slice(ends[e], ends[e + 1])
+            if ends[e + 1] > ends[e]:
+                check(y[own], *product64(x[rows.long()[own]], W[e], b[e], RELU))
+                f[own], tol[own] = product64(y[own], W2[e], b2[e], NONE)
+        assert (y[ends[-1]:] == 7).all()
+        there, pick = (slots >= 0)[:, :, None], slots.long().clamp(min=0)
+        part = torch.where(there, f[pick] * w.double()[:, :, None], 0.0)
+        check(back, part.sum(1), (torch.where(there, tol[pick] * w.double()[:, :, None], 0.0) + 2.0 ** -22 * part.abs()).sum(1))
+
+
+@gpu
 @pytest.mark.parametrize("n", [1, 4, 8, 20, 200])
 def test_weights_and_rows_written_by_the_launch_before(n):
     """A launch begins while the one before is still running: weights, rows and slots that that one writes, at the same place every time, are read as written."""
@@ -196,6 +248,42 @@ def test_weights_and_rows_written_by_the_launch_before(n):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for i in range(rounds) for p, q in zip(apart[i], together[i]))
+
+
+# ---- router -----------------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("tokens,experts,top_k", [(1, 1024, 32), (100, 1024, 32), (128, 600, 7), (77, 300, 20), (128, 129, 1), (90, 128, 16), (200, 128, 16), (300, 64, 9), (130, 600, 32)])
+@pytest.mark.parametrize("normalise", [True, False])
+def test_route_of_many_experts(tokens, experts, top_k, normalise):
+    g = torch.Generator(device="cuda").manual_seed(tokens + experts)
+    logits = torch.randn(tokens, experts, generator=g, device="cuda") * 4
+    check_route(logits, top_k, normalise)
+    logits = torch.round(logits)
+    logits[torch.rand(tokens, experts, generator=g, device="cuda") < 0.9] = -math.inf
+    check_route(logits, top_k, normalise)
+
+
+@gpu
+@pytest.mark.parametrize("tokens,experts,top_k", [(65537, 64, 4), (70001, 8, 2), (150001, 5, 1), (300007, 100, 3), (40000, 200, 8)])
+def test_route_of_very_many_tokens(tokens, experts, top_k):
+    """Parts of 64, 128, 256 and more tokens; checked in whole-array form, with masked tokens."""
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    logits = torch.randn(tokens, experts, generator=g, device="cuda")
+    logits[tokens - tokens // 9:] = -math.inf
+    logits[1000] = -math.inf
+    chosen, w, off, rows, slots = T.tardis_route(logits, top_k)
+    top, idx = logits.sort(dim=1, descending=True, stable=True)
+    there = top[:, :top_k] > -math.inf
+    want = torch.where(there, idx[:, :top_k], experts)
+    assert torch.equal(torch.where(chosen >= 0, chosen, experts).long(), want)
+    order = torch.argsort(want.reshape(-1), stable=True)
+    pairs = int(there.sum())
+    assert torch.equal(rows.long()[:pairs], order[:pairs] // top_k) and (rows[pairs:] == -1).all()
+    assert torch.equal(slots.reshape(-1).long()[order[:pairs]], torch.arange(pairs, device="cuda")) and (slots[~there] == -1).all()
+    assert off.tolist() == [0] + torch.bincount(want.reshape(-1), minlength=experts)[:experts].cumsum(0).tolist()
+    share = torch.where(there, torch.exp((top[:, :top_k] - top[:, :1]).double()), 0.0)
+    ref = torch.where(there, share / share.sum(1, keepdim=True), 0.0)
+    assert ((w.double() - ref).abs() <= 45 * 2.0 ** -24 * ref + 1e-37).all()
 
 
 # ---- the binding ------------------------------------------------------------------------------------------------
