@@ -160,8 +160,8 @@ __global__ void __launch_bounds__(256) k_linear_few_f32(const __grid_constant__ 
     for (int i = 0; i < O; ++i) wv[i] = *reinterpret_cast<const float4*>(w[i] + k);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      if (!there[r]) continue;
-      const float4 xv = *reinterpret_cast<const float4*>(x[r] + k);
+      if (r >= t.rows) continue;
+      const float4 xv = there[r] ? *reinterpret_cast<const float4*>(x[r] + k) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < O; ++i) acc[i][r] = fmaf(wv[i].w, xv.w, fmaf(wv[i].z, xv.z, fmaf(wv[i].y, xv.y, fmaf(wv[i].x, xv.x, acc[i][r]))));
     }

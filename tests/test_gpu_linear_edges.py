@@ -172,6 +172,23 @@ def test_experts_without_rows_choose_no_other_kernel(n, experts, o):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,o", [(1, 40), (3, 40), (7, 40), (20, 40), (100, 520), (1500, 4104)])
+def test_rows_outside_x_are_rows_of_zeros(n, o, dtype):
+    """Times infinite weights they are NaN, as zeros of x are, whichever kernel serves the call; times finite ones the bias."""
+    k = 72
+    x, W, b, _ = make(n, k, o, dtype, groups=1)
+    W[0, 5, 3] = math.inf
+    rows = torch.arange(n, dtype=torch.int32, device="cuda")
+    rows[n // 2] = -1
+    for out in {dtype, F32}:
+        y = T.tardis_grouped_linear(x, W, torch.tensor([0, n], dtype=torch.int32, device="cuda"), bias=b, rows=rows, out_dtype=out)[n // 2]
+        assert y[5].isnan()
+        y[5] = b[0, 5]
+        assert torch.equal(y, b[0].to(out))
+
+
+@gpu
 def test_group_sizes_change_between_replays():
     """One captured call; the sizes of the groups, the rows and the slots change on the device: even, all in one group, skewed, none."""
     tokens, experts, top_k, k, o = 700, 6, 2, 136, 4104
