@@ -259,7 +259,7 @@ def tardis_linear(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor]
                   residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype=None, stream=None):
     """y = act(x W^T + bias) + residual in one launch (see tardis_linear in tardis.h): x [n, k], W [o, k] float32 or bfloat16
     with unit inner stride, bias [o] float32, residual and y [n, o] in out_dtype (x's dtype, or float32).  Returns y (`out`
-    when given; it may be the residual)."""
+    when given; it may be the residual).  No gradient is recorded, here and in the calls below."""
     if x.dim() != 2 or W.dim() != 2 or W.shape[1] != x.shape[1]:
         raise TardisError(1, "x must be [n, k] and W [o, k]")
     _check_act(act)

@@ -365,8 +365,8 @@ k_linear_tc(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   } else if (GATHER && warp >= NTHREADS / 32) {
     // ---------------- rows of x by their indices ----------------
     // Each of four warps has a quarter of this CTA's rows, their indices in registers that all lanes hold alike, and copies them four at a time.
-    // (8192 rows of 8 experts, 4096 -> 16384: 898 us; issued by the 32 lanes of one warp 2490, 80 cycles each; copied by threads, whose writes need a fence towards the
-    // tensor cores, 2040.)
+    // (Issued by the 32 lanes of one warp, 80 cycles each, 8192 rows of 8 experts, 4096 -> 16384, took 2.8 times as long; copied by threads, whose writes need a fence towards
+    // the tensor cores, 2.3 times.)
     constexpr int QUADS = C::B_ROWS / (4 * GATHER_WARPS);
     const int w = warp - NTHREADS / 32;
     int s = 0, parity = 1;
@@ -684,8 +684,9 @@ tardis_status_t launch_linear_tc(const LinearArgs& given, cudaStream_t s) {
   TARDIS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   const Choice best = choose(a, sms);
   if (best.kind == 2) {
-    // Every tile of 256 outputs picks its rows again, at a third of the rate of whole boxes: with scratch and many outputs they are picked once (8192 rows of 4096 -> 16384:
-    // 957 us picked tile by tile, 762 picked before; 3800 rows of 16 experts 8192 -> 2048, where the weights of small groups take as long, 170 and 185).
+    // Every tile of 256 outputs picks its rows again, at a third of the rate of whole boxes: with scratch and many outputs they are picked once (us picked tile by tile / once:
+    // 8192 rows of 8 experts 4096 -> 16384 1008 / 835, -> 4096 262 / 235, -> 2048 133 / 128; 4000 rows of 16 experts 8192 -> 4224 359 / 339, -> 2048, where the weights of
+    // small groups take as long, 170 / 175).
     if (a.rows && a.work && a.o >= 4096) {
       const tardis_status_t st = launch_gather_rows(a, s);
       if (st != TARDIS_OK) return st;
