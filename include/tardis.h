@@ -222,8 +222,8 @@ tardis_status_t tardis_linear(const tardis_linear_desc_t* desc, tardis_stream_t 
  *   rows       device [n_rows] or NULL; an index outside 0 .. n_x - 1 reads as a row of zeros;
  *   W          [n_experts][o, k]: experts stride_w elements apart (a multiple of 8, at least (o - 1) ldw + k);
  *   work       device scratch, 16-byte aligned, caller-owned (calls that overlap in time need one each).  With slots at
- *              least 4 n_rows o8 bytes, o8 = o rounded up to a multiple of 8.  Else it may be NULL; with rows, bf16 operands and outputs, at
- *              least 4096 outputs and 2 n_rows k bytes of scratch, long calls gather the rows there once instead of picking them again for
+ *              least 4 n_rows o8 bytes, o8 = o rounded up to a multiple of 8.  Else it may be NULL; with rows, bf16 operands and outputs, up to
+ *              2^17 channels, at least 4096 outputs and 2 n_rows k bytes of scratch, long calls gather the rows there once instead of picking them again for
  *              every tile of outputs (calls with fp32 outputs never do: their tiles are not those of pairs of CTAs).  It
  *              overlaps no other array.
  * Other arguments, alignment, result and errors as for tardis_linear; n_experts <= 1024 (UNSUPPORTED beyond). */

@@ -305,7 +305,7 @@ def _grouped(x, W, offsets, bias, act, rows, residual, out, out_dtype, back, wor
         elif work.get_device() != index or not work.is_contiguous() or work.numel() * work.element_size() < room:
             raise TardisError(1, "work must be a contiguous tensor of at least 4 rows o bytes (o rounded up to 8) on x's device")
         pwork = work.data_ptr()
-    elif rows is not None and n >= 1024 and o >= 4096 and dtype is torch.bfloat16 and out_dtype is torch.bfloat16:       # (where long calls use it)
+    elif rows is not None and n >= 1024 and o >= 4096 and k <= 1 << 17 and dtype is torch.bfloat16 and out_dtype is torch.bfloat16:      # (where long calls use it)
         work, room = _empty(x, (n, k), dtype, stream), 2 * n * k
         pwork = work.data_ptr()
     if out is None:                                          # (rows in no group are left as they were: zero)

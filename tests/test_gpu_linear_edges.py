@@ -318,12 +318,12 @@ def test_rows_in_no_group_of_a_fresh_output_are_zero(dtype):
 
 
 @gpu
-def test_no_scratch_for_calls_that_use_none():
-    """fp32 outputs pick their rows tile by tile: n k bf16 of scratch would never be touched."""
-    n, k, o = 2048, 4096, 4096
+@pytest.mark.parametrize("n,k,o,out", [(2048, 4096, 4096, F32), (1024, 2 ** 17 + 8, 4096, BF)])
+def test_no_scratch_for_calls_that_use_none(n, k, o, out):
+    """fp32 outputs, and 16-bit ones of very many channels, pick their rows tile by tile: n k bf16 of scratch would never be touched."""
     x, W, _, _ = make(n, k, o, BF, groups=1)
     rows, off = torch.arange(n, dtype=torch.int32, device="cuda"), torch.tensor([0, n], dtype=torch.int32, device="cuda")
-    y = torch.empty(n, o, device="cuda")
+    y = torch.empty(n, o, dtype=out, device="cuda")
     T.tardis_grouped_linear(x, W, off, rows=rows, out=y)
     torch.cuda.synchronize()
     torch.cuda.reset_peak_memory_stats()
